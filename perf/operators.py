@@ -235,7 +235,6 @@ def _prepare_own(s):
     ptr = np.arange(hosts + 1, dtype=np.int32) if hosts > 1 else np.zeros(2, dtype=np.int32)
     s["topo"] = a2a.Topology(ptr, (ring + 1) % hosts if hosts > 1 else ring[:0])
     T, X = s["case"]["tokens"], s["experts"]
-    s["ws"] = s["topo"].alloc_dispatch_workspace(hosts, tokens=T, choices_per_token=s["k"], experts=X)
     if call == "demand":
         s["demand"] = buffer(hosts, hosts, dtype=torch.float64)
         return
@@ -243,6 +242,7 @@ def _prepare_own(s):
     if call != "counts":
         s["loss"], s["prob_sums"] = buffer(1), buffer(hosts, X)
         s["rows"] = buffer(hosts, dtype=torch.int32)
+        s["ws"] = s["topo"].alloc_balance_workspace(hosts, tokens=T, experts=X)
     if call == "loss_grad":
         s["grad"] = torch.empty_like(s["logits"])
 
@@ -262,11 +262,11 @@ def _run_own(s):
         return {"cost": s["out"]}
     routing = dict(choices=s["choices"], host_begin=s["host_begin"], experts=s["experts"])
     if call == "counts":
-        topo.dispatch_counts(hosts, counts=s["counts"], workspace=s["ws"], **routing)
+        topo.dispatch_counts(hosts, counts=s["counts"], **routing)
         return {"counts": s["counts"]}
     if call == "demand":
         topo.dispatch_demand(hosts, expert_host=s["expert_host"], once=s["case"]["once"], demand=s["demand"],
-                             workspace=s["ws"], **routing)
+                             **routing)
         return {"demand": s["demand"]}
     weights = dict(cost=s["cost"], expert_host=s["expert_host"] if s["cost"] is not None else None)
     topo.balance_loss(hosts, logits=s["logits"], choices=s["choices"], host_begin=s["host_begin"], loss=s["loss"],
