@@ -19,8 +19,8 @@
  *     out- and in-neighbour CSR, as much pinned host memory).  The memory of up to four destroyed small
  *     handles (2 MiB each at most) is kept for the next ones.
  *   - All device work is enqueued on `hip_stream` (a hipStream_t passed as void*; NULL = the
- *     default stream).  a2a_distances, a2a_link_loads, a2a_link_loads_demand and
- *     a2a_link_loads_static only enqueue kernels of this library: they never wait for the device,
+ *     default stream).  a2a_distances, a2a_link_loads, a2a_link_loads_demand, a2a_link_loads_static,
+ *     a2a_path_costs and the dispatch functions only enqueue kernels of this library: they never wait for the device,
  *     copy nothing to the host and allocate nothing, so they return while earlier work on the
  *     stream may still be running, and a stream under HIP graph capture records them (the launch
  *     sequence depends only on the handle, the source range and the workspace size; what depends
@@ -34,7 +34,7 @@
  *     aborts or prints.  On error the outputs are unspecified.
  *   - Sources are processed in batches of 64 (one bit of a 64-bit mask per source); several
  *     batches advance level by level together, as many as the workspace holds.
- *   - All arithmetic is in double precision.  Inside the workspace and the kernels path counts
+ *   - All arithmetic on topologies is in double precision.  Inside the workspace and the kernels path counts
  *     are kept in less (floats, whole numbers of 12, 13 or 24 bits) while (largest
  *     in-degree)^level says that every one of them is a whole number that fits, or with a place
  *     for the exact count of those that do not; results do not depend on it.
@@ -68,6 +68,7 @@ typedef enum a2a_status {
 #define A2A_WS_SIGMA 0x1     /* a2a_distances with sigma */
 #define A2A_WS_LOADS 0x2     /* a2a_link_loads */
 #define A2A_WS_SSSP 0x4      /* a2a_sssp_loads; pass iter_sources as src_count */
+#define A2A_WS_COSTS 0x8     /* a2a_path_costs */
 #define A2A_WS_MINIMAL 0x100 /* smallest usable size (one batch at a time) instead of the
                                 recommended one (all batches advance together) */
 
@@ -207,6 +208,110 @@ int a2a_sssp_loads(const a2a_topo* topo, int32_t src_begin, int32_t src_count, i
                    double* load, int64_t* dist_sum_total, int64_t* flags, void* workspace,
                    size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Mean cost of the shortest paths of every pair whose source lies in src_begin .. src_begin+src_count-1:
+ *   cost(s,t) = 1/sigma(s,t) * sum over the shortest s->t paths of the sum of link_cost[a] over their links,
+ * which is what a unit of demand(s,t) costs when it is split equally over those paths (Sec. 5.2) and link a takes
+ * link_cost[a] a unit.  It is the gradient of sum_a link_cost[a] * load[a] by demand(s,t), with load as
+ * a2a_link_loads_demand computes it: sum_a link_cost[a] * load[a] = sum_{s,t} demand(s,t) * cost(s,t).  With the same
+ * cost 1 for every link it is D(s,t).
+ *   dist       device, int32[src_count][N], and
+ *   sigma      device, double[src_count][N]: as a2a_distances leaves them for these sources.  Read only.  (Other
+ *              values give other costs, never an access out of bounds.)
+ *   link_cost  device, double[E], by link id; any finite numbers.  NULL: 1 for every link
+ *   cost       device, double[src_count][N], row-major, overwritten; 0 where t = s or t cannot be reached
+ *   workspace  device, a2a_workspace_bytes(topo, src_count, A2A_WS_COSTS) bytes, 256-byte aligned
+ * Only enqueues, like a2a_link_loads.  Every sum is taken in a fixed order.
+ */
+int a2a_path_costs(const a2a_topo* topo, int32_t src_begin, int32_t src_count, const int32_t* dist, const double* sigma,
+                   const double* link_cost, double* cost, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The all-to-all of a mixture-of-experts layer.  Its tokens lie on hosts, so do its experts, and a router has chosen
+ * some experts for every token: that is who sends how much to whom.  The functions below take the router's output as it
+ * lies on the device.  They only enqueue, like a2a_link_loads, and their results are the same bits from run to run.
+ * They count in whole numbers; logits, probabilities and their sums are single precision.  Sources here are the
+ * consecutive groups of tokens that host_begin says: hosts, or for a2a_dispatch_counts and the balance loss whatever a
+ * program groups tokens by (sequences, one group for all).
+ */
+typedef enum a2a_type { A2A_F32 = 0, A2A_BF16 = 1, A2A_F16 = 2, A2A_I32 = 3, A2A_I64 = 4 } a2a_type;
+
+typedef struct a2a_routing {
+  int64_t tokens;             /* >= 0 */
+  int32_t choices_per_token;  /* 1 .. 64; tokens * choices_per_token < 2^31 */
+  int32_t experts;            /* >= 1 */
+  int32_t choices_type;       /* A2A_I32 or A2A_I64 */
+  int32_t reserved;           /* 0 */
+  const void* choices;        /* device: token t's choices are the choices_per_token numbers from
+                                 choices[t * choices_stride] on; a number outside [0, experts) is none
+                                 (a dropped choice, a padded token).  Aligned to its type. */
+  int64_t choices_stride;     /* in numbers, >= choices_per_token */
+  const int64_t* host_begin;  /* device, int64[src_count + 1], non-decreasing: source s has the tokens
+                                 host_begin[s] .. host_begin[s+1]-1.  Tokens before host_begin[0], from
+                                 host_begin[src_count] on and outside 0 .. tokens-1 belong to no source. */
+  const int32_t* expert_host; /* device, int32[experts]: the host of each expert; a number outside [0, N)
+                                 is none, the expert is sent nothing.  NULL: expert e lies on host e. */
+} a2a_routing;
+
+/*
+ * How many choices of each source's tokens fall on each expert.  (A number that one token has twice counts twice.)
+ *   counts  device, int32[src_count][experts], overwritten
+ * expert_host is not used.
+ */
+int a2a_dispatch_counts(const a2a_topo* topo, int32_t src_count, const a2a_routing* routing, int32_t* counts,
+                        void* hip_stream);
+
+/*
+ * The demands of the dispatch, in tokens: what a2a_link_loads_demand takes for src_count sources (its src_begin is the
+ * host of the first).
+ *   once    0: every choice is a token sent.  1: a token goes to a host once, however many of its choices are there.
+ *   demand  device, double[N][src_count], by target, overwritten: whole numbers
+ * src_count <= N.
+ */
+int a2a_dispatch_demand(const a2a_topo* topo, int32_t src_count, const a2a_routing* routing, int once, double* demand,
+                        void* hip_stream);
+
+/*
+ * Balance loss of a router, its probabilities weighted by what a source pays to reach an expert.  With
+ * p_t = softmax(logits_t) over the X experts, a row whose logits are all -infinity being no token (nothing of it counts,
+ * its choices neither), and over the tokens of source s
+ *   rows_s = how many, counts[s][e] = choices of e, prob_sums[s][e] = sum_t p_t[e], n = sum_s rows_s,
+ *   loss = X / (k n) * sum_s 1/rows_s * sum_e weight(s,e) * counts[s][e] * prob_sums[s][e]
+ * (k = choices_per_token; sources without rows add nothing; 0 without any).  With one source and weight 1 it is the
+ * usual X * sum_e (share of choices) * (mean probability), 1 for a router in balance.  With a2a_path_costs or hop
+ * distances for weights it is the traffic that the router's probabilities ask of the links.
+ *   logits      device, tokens rows of `experts` numbers, logits_stride apart (>= experts), of logits_type
+ *               (A2A_F32, A2A_BF16 or A2A_F16).  -infinity for experts that a token must not take.  A row with a NaN
+ *               or +infinity makes its source's sums, and the loss, NaN.
+ *   cost        device, double[src_count][N]: weight(s,e) = cost[s][expert_host[e]], 0 for an expert without a host.
+ *               NULL: weight 1, expert_host is not used.
+ *   loss        device, float[1]
+ *   counts      device, int32[src_count][experts]
+ *   prob_sums   device, float[src_count][experts]
+ *   rows        device, int32[src_count]
+ *               All four overwritten; a2a_balance_loss_grad reads counts and rows.
+ *   workspace   device, a2a_balance_workspace_bytes(...) bytes, 256-byte aligned
+ * A2A_ERR_NOT_IMPLEMENTED for more than A2A_MOST_EXPERTS experts.
+ */
+#define A2A_MOST_EXPERTS 4096
+size_t a2a_balance_workspace_bytes(const a2a_topo* topo, int32_t src_count, int64_t tokens, int32_t experts);
+int a2a_balance_loss(const a2a_topo* topo, int32_t src_count, const a2a_routing* routing, const void* logits,
+                     int logits_type, int64_t logits_stride, const double* cost, float* loss, int32_t* counts,
+                     float* prob_sums, int32_t* rows, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Its gradient by the logits, with the choices taken as they are (counts are constants):
+ *   grad_t[e] = upstream * p_t[e] * (c[s][e] - sum_f p_t[f] c[s][f]),  c[s][e] = X weight(s,e) counts[s][e] / (k n rows_s)
+ *   routing     tokens, choices_per_token, experts, host_begin and expert_host are used, choices is not
+ *   counts, rows  as a2a_balance_loss left them.  Read only.
+ *   upstream    device, float[1]: gradient by the loss.  NULL: 1
+ *   grad        device, like logits (logits_type), rows grad_stride apart (>= experts).  Rows of tokens that belong to
+ *               no source are left as they are; rows of no token (all -infinity) are 0.  May be the logits themselves.
+ */
+int a2a_balance_loss_grad(const a2a_topo* topo, int32_t src_count, const a2a_routing* routing, const void* logits,
+                          int logits_type, int64_t logits_stride, const double* cost, const int32_t* counts,
+                          const int32_t* rows, const float* upstream, void* grad, int64_t grad_stride, void* hip_stream);
+
 typedef struct a2a_bound {
   double max_load;         /* Lmax: all-to-all time under unit demand and capacity (Sec. 5.3) */
   int64_t argmax_arc;      /* lowest link id whose load equals max_load */
@@ -325,6 +430,7 @@ typedef enum a2a_prof_kernel {
   A2A_K_EXTRACT,   /* dist / sigma output of a2a_distances (level kernels) */
   A2A_K_SEARCH,    /* search of all levels with its state in LDS (a2a_distances: and the output of dist) */
   A2A_K_SOURCES,   /* a workgroup's sources from the search (or its levels) to their results, in LDS */
+  A2A_K_TOKENS,    /* passes over a router's tokens, and the sums behind them */
   A2A_K_COUNT
 } a2a_prof_kernel;
 #define A2A_PROF_MAX_LEVELS 64 /* deeper levels are lumped into the last slot */

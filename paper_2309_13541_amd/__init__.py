@@ -10,6 +10,7 @@ from .binding import (  # noqa: F401
     BoundCap,
     Profile,
     PROF_KERNELS,
+    Routing,
     Topology,
     TreeBound,
     tree_lower_bound,
@@ -19,7 +20,8 @@ from .binding import (  # noqa: F401
     status_string,
     EXPORTED_SYMBOLS,
     STATIC_WORKSPACE_BYTES,
-    WS_DISTANCES, WS_SIGMA, WS_LOADS, WS_SSSP, WS_MINIMAL,
+    MOST_EXPERTS,
+    WS_DISTANCES, WS_SIGMA, WS_LOADS, WS_SSSP, WS_COSTS, WS_MINIMAL,
     FLAG_SIGMA_INEXACT, FLAG_UNREACHABLE,
     OK, ERR_INVALID_ARG, ERR_SELF_LOOP, ERR_WORKSPACE_TOO_SMALL, ERR_HIP, ERR_NOT_IMPLEMENTED,
     ERR_DISCONNECTED, ERR_NO_MEMORY, ERR_LEVEL_OVERFLOW,

@@ -34,6 +34,7 @@ WS_DISTANCES = 0x0
 WS_SIGMA = 0x1
 WS_LOADS = 0x2
 WS_SSSP = 0x4
+WS_COSTS = 0x8
 WS_MINIMAL = 0x100
 FLAG_SIGMA_INEXACT = 0x1
 FLAG_UNREACHABLE = 0x2
@@ -42,12 +43,14 @@ EXPORTED_SYMBOLS = (
     "a2a_topo_create", "a2a_topo_destroy", "a2a_topo_info", "a2a_workspace_bytes",
     "a2a_distances", "a2a_link_loads", "a2a_link_loads_demand", "a2a_schedule_bound", "a2a_status_string",
     "a2a_profile_enable", "a2a_profile_read", "a2a_tree_lower_bound", "a2a_schedule_bound_cap",
-    "a2a_link_loads_static", "a2a_sssp_loads",
+    "a2a_link_loads_static", "a2a_sssp_loads", "a2a_path_costs", "a2a_dispatch_counts", "a2a_dispatch_demand",
+    "a2a_balance_workspace_bytes", "a2a_balance_loss", "a2a_balance_loss_grad",
 )
+MOST_EXPERTS = 4096
 STATIC_WORKSPACE_BYTES = 32 << 20
 
 PROF_KERNELS = ("init", "bfs", "offsets", "fwd_rows", "fwd_few", "fwd_spread", "bwd_rows", "bwd_few", "bwd_spread",
-                "reduce", "extract", "search", "sources")
+                "reduce", "extract", "search", "sources", "tokens")
 PROF_MAX_LEVELS = 64
 
 HIPCC_FLAGS = [
@@ -117,6 +120,13 @@ class Profile(ctypes.Structure):
         return d
 
 
+class Routing(ctypes.Structure):
+    """Mirror of ``a2a_routing``."""
+    _fields_ = [("tokens", ctypes.c_int64), ("choices_per_token", ctypes.c_int32), ("experts", ctypes.c_int32),
+                ("choices_type", ctypes.c_int32), ("reserved", ctypes.c_int32), ("choices", ctypes.c_void_p),
+                ("choices_stride", ctypes.c_int64), ("host_begin", ctypes.c_void_p), ("expert_host", ctypes.c_void_p)]
+
+
 def library_path() -> str:
     return _LIB
 
@@ -183,6 +193,18 @@ def load_library():
     lib.a2a_sssp_loads.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.a2a_link_loads_demand.restype = ctypes.c_int
     lib.a2a_link_loads_demand.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.a2a_path_costs.restype = ctypes.c_int
+    lib.a2a_path_costs.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.a2a_dispatch_counts.restype = ctypes.c_int
+    lib.a2a_dispatch_counts.argtypes = [vp, i32, ctypes.POINTER(Routing), vp, vp]
+    lib.a2a_dispatch_demand.restype = ctypes.c_int
+    lib.a2a_dispatch_demand.argtypes = [vp, i32, ctypes.POINTER(Routing), ctypes.c_int, vp, vp]
+    lib.a2a_balance_workspace_bytes.restype = sz
+    lib.a2a_balance_workspace_bytes.argtypes = [vp, i32, i64, i32]
+    lib.a2a_balance_loss.restype = ctypes.c_int
+    lib.a2a_balance_loss.argtypes = [vp, i32, ctypes.POINTER(Routing), vp, ctypes.c_int, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.a2a_balance_loss_grad.restype = ctypes.c_int
+    lib.a2a_balance_loss_grad.argtypes = [vp, i32, ctypes.POINTER(Routing), vp, ctypes.c_int, i64, vp, vp, vp, vp, vp, i64, vp]
     lib.a2a_schedule_bound_cap.restype = ctypes.c_int
     lib.a2a_schedule_bound_cap.argtypes = [vp, vp, vp, i64, i64, ctypes.c_double, ctypes.c_double, vp, vp]
     lib.a2a_schedule_bound.restype = ctypes.c_int
@@ -220,6 +242,49 @@ def _check(status: int, where: str, allow=()):
 
 def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+# a2a_type of a torch type, by its name (torch is imported when the library is loaded)
+_TYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2, "torch.int32": 3, "torch.int64": 4}
+_type_codes = {}
+
+
+def _type_code(dtype) -> int:
+    code = _type_codes.get(dtype)
+    if code is None:
+        code = _type_codes[dtype] = _TYPES.get(str(dtype), -1)
+    return code
+
+
+def _refuse(where: str, why: str):
+    raise A2AError(ERR_INVALID_ARG, f"{where}: {why}")
+
+
+def _whole(where: str, name: str, t, dtype: str, shape) -> int:
+    """Address of a contiguous device tensor of that type and shape."""
+    if str(t.dtype) != dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        _refuse(where, f"{name} has to be a contiguous {dtype} device tensor of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _rows(where: str, name: str, t, codes):
+    """Type and distance of the rows of a device matrix whose numbers lie next to each other in a row."""
+    code = _type_code(t.dtype)
+    if code not in codes or t.dim() != 2 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1 and t.numel() > 0):
+        _refuse(where, f"{name} has to be a device matrix of one of the types in the header, its rows' numbers next to each other")
+    return code, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _routing(where: str, src_count: int, host_begin, experts: int, expert_host, *, choices=None, tokens=0, choices_per_token=0):
+    r = Routing(tokens, choices_per_token, experts)
+    if choices is not None:
+        r.choices_type, r.choices_stride = _rows(where, "choices", choices, (3, 4))
+        r.tokens, r.choices_per_token = choices.shape
+        r.choices = choices.data_ptr()
+    r.host_begin = _whole(where, "host_begin", host_begin, "torch.int64", (src_count + 1,))
+    if expert_host is not None:
+        r.expert_host = _whole(where, "expert_host", expert_host, "torch.int32", (experts,))
+    return r
 
 
 def _stream(stream) -> Optional[int]:
@@ -299,6 +364,86 @@ class Topology:
             self._h, src_begin, src_count, _ptr(demand), _ptr(load), _ptr(weighted_dist), _ptr(dist_sum_total),
             _ptr(flags), _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream(stream)),
             "a2a_link_loads_demand")
+
+    def path_costs(self, src_begin: int, src_count: int, *, dist, sigma, link_cost=None, cost, workspace, stream=None) -> int:
+        """a2a_path_costs: ``dist`` and ``sigma`` as :meth:`distances` leaves them, ``link_cost`` float64 [E] (None: 1 each),
+        ``cost`` float64 [src_count][N]: mean cost of the shortest paths, the gradient of ``(link_cost * load).sum()`` by
+        the demands of :meth:`link_loads_demand` (there by target, here by source)."""
+        where, shape = "a2a_path_costs", (src_count, self.N)
+        return _check(load_library().a2a_path_costs(
+            self._h, src_begin, src_count, _whole(where, "dist", dist, "torch.int32", shape),
+            _whole(where, "sigma", sigma, "torch.float64", shape),
+            None if link_cost is None else _whole(where, "link_cost", link_cost, "torch.float64", (self.E,)),
+            _whole(where, "cost", cost, "torch.float64", shape), _ptr(workspace),
+            workspace.numel() if workspace is not None else 0, _stream(stream)), where)
+
+    def dispatch_counts(self, src_count: int, *, choices, host_begin, experts: int, counts, stream=None) -> int:
+        """a2a_dispatch_counts: how many of the ``choices`` (int32 or int64 [tokens][k]) of each source's tokens fall on
+        each expert.  Source s has the tokens ``host_begin[s]`` to ``host_begin[s + 1] - 1`` (int64 [src_count + 1]).
+        ``counts``: int32 [src_count][experts]."""
+        where = "a2a_dispatch_counts"
+        r = _routing(where, src_count, host_begin, experts, None, choices=choices)
+        return _check(load_library().a2a_dispatch_counts(
+            self._h, src_count, r, _whole(where, "counts", counts, "torch.int32", (src_count, experts)), _stream(stream)), where)
+
+    def dispatch_demand(self, src_count: int, *, choices, host_begin, experts: int, expert_host=None, once: bool = False,
+                        demand, stream=None) -> int:
+        """a2a_dispatch_demand: what each source sends to each host, ``demand`` of :meth:`link_loads_demand` (float64
+        [N][src_count]), in tokens.  Expert e lies on host ``expert_host[e]`` (int32; None: on host e); ``once``: a token goes
+        to a host once, however many of its choices are there."""
+        where = "a2a_dispatch_demand"
+        r = _routing(where, src_count, host_begin, experts, expert_host, choices=choices)
+        return _check(load_library().a2a_dispatch_demand(
+            self._h, src_count, r, int(once), _whole(where, "demand", demand, "torch.float64", (self.N, src_count)),
+            _stream(stream)), where)
+
+    def balance_workspace_bytes(self, src_count: int, *, tokens: int, experts: int) -> int:
+        return int(load_library().a2a_balance_workspace_bytes(self._h, src_count, tokens, experts))
+
+    def alloc_balance_workspace(self, src_count: int, *, tokens: int, experts: int):
+        """A torch uint8 device tensor for :meth:`balance_loss`."""
+        import torch
+        return torch.empty(self.balance_workspace_bytes(src_count, tokens=tokens, experts=experts), dtype=torch.uint8,
+                           device="cuda")
+
+    def balance_loss(self, src_count: int, *, logits, choices, host_begin, cost=None, expert_host=None, loss, counts,
+                     prob_sums, rows, workspace, stream=None) -> int:
+        """a2a_balance_loss: ``loss`` (float32 [1]) of a router with ``logits`` (float32, bfloat16 or float16
+        [tokens][experts]) that made ``choices``, weighted by ``cost`` (float64 [src_count][N]; None: 1 each); and, for the
+        gradient, ``counts`` (int32 [src_count][experts]), ``prob_sums`` (float32, the same) and ``rows`` (int32 [src_count])."""
+        where = "a2a_balance_loss"
+        kind, stride = _rows(where, "logits", logits, (0, 1, 2))
+        tokens, experts = logits.shape
+        r = _routing(where, src_count, host_begin, experts, expert_host, choices=choices)
+        if r.tokens != tokens:
+            _refuse(where, "logits and choices have to have as many rows")
+        shape = (src_count, experts)
+        return _check(load_library().a2a_balance_loss(
+            self._h, src_count, r, logits.data_ptr(), kind, stride,
+            None if cost is None else _whole(where, "cost", cost, "torch.float64", (src_count, self.N)),
+            _whole(where, "loss", loss, "torch.float32", (1,)), _whole(where, "counts", counts, "torch.int32", shape),
+            _whole(where, "prob_sums", prob_sums, "torch.float32", shape),
+            _whole(where, "rows", rows, "torch.int32", (src_count,)), _ptr(workspace),
+            workspace.numel() if workspace is not None else 0, _stream(stream)), where)
+
+    def balance_loss_grad(self, src_count: int, *, logits, choices_per_token: int, host_begin, cost=None, expert_host=None,
+                          counts, rows, upstream=None, grad, stream=None) -> int:
+        """a2a_balance_loss_grad: gradient of :meth:`balance_loss` by the logits, ``grad`` (like ``logits``), times
+        ``upstream`` (float32 [1]; None: 1)."""
+        where = "a2a_balance_loss_grad"
+        kind, stride = _rows(where, "logits", logits, (0, 1, 2))
+        grad_stride = _rows(where, "grad", grad, (kind,))[1]
+        tokens, experts = logits.shape
+        if grad.shape != logits.shape:
+            _refuse(where, "grad has to have the shape of logits")
+        r = _routing(where, src_count, host_begin, experts, expert_host, tokens=tokens, choices_per_token=choices_per_token)
+        return _check(load_library().a2a_balance_loss_grad(
+            self._h, src_count, r, logits.data_ptr(), kind, stride,
+            None if cost is None else _whole(where, "cost", cost, "torch.float64", (src_count, self.N)),
+            _whole(where, "counts", counts, "torch.int32", (src_count, experts)),
+            _whole(where, "rows", rows, "torch.int32", (src_count,)),
+            None if upstream is None else _whole(where, "upstream", upstream, "torch.float32", (1,)),
+            grad.data_ptr(), grad_stride, _stream(stream)), where)
 
     def profile_enable(self, mode: int = 1) -> None:
         """0 off, 1 events around the launches, 2 the same of the level kernels, which then serve every topology, and

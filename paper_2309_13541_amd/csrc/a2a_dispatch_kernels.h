@@ -1,0 +1,377 @@
+// Device code of the dispatch functions: counts and demands of a router's choices, the balance loss and its gradient.
+#pragma once
+
+#include "a2a_dispatch_plan.h"
+#include "a2a_kernels.h"
+
+namespace a2a_dev {
+
+// ---------------------------------------------------------------------------------------
+// tokens and their sources
+// ---------------------------------------------------------------------------------------
+
+struct Routing {
+  const void* choices;
+  const int64_t* host_begin;
+  const int32_t* expert_host;
+  long long tokens, stride;
+  int k, experts, sources;
+};
+
+// Entries of host_begin that are at most t: the source of token t is one less.  Of all lanes together, 64 parts of what
+// is left at a time: three steps for up to 262143 sources.
+__device__ __forceinline__ int begun(const int64_t* __restrict__ begin, int entries, long long t) {
+  int lo = 0, hi = entries;
+  while (lo < hi) {
+    const int part = (hi - lo + kWave - 1) / kWave;
+    const int at = min(lo + (lane_id() + 1) * part, hi) - 1;
+    const int whole = __popcll(__ballot(begin[at] <= t && lo + lane_id() * part < hi));
+    // all of the parts before the first whose last entry is larger (of a last, shorter part too)
+    if (lo + whole * part >= hi) return hi;
+    lo += whole * part;
+    hi = min(lo + part, hi) - 1;
+  }
+  return lo;
+}
+
+// ---------------------------------------------------------------------------------------
+// counts and demands
+// ---------------------------------------------------------------------------------------
+
+template <typename Id>
+__device__ __forceinline__ int host_of(const Routing& r, long long t, int j, int hosts) {
+  const Id e = ((const Id*)r.choices)[t * r.stride + j];
+  if (e < 0 || e >= r.experts) return -1;
+  const int h = r.expert_host ? r.expert_host[e] : (int)e;
+  return h >= 0 && h < hosts ? h : -1;
+}
+
+static __global__ void __launch_bounds__(kBlock) k_fill(int32_t* p, size_t n) {
+  for (size_t i = (size_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += (size_t)gridDim.x * kBlock) p[i] = 0;
+}
+
+// A thread per choice, and an atomic addition for each.  Whole numbers below 2^53: the order does not matter.
+template <typename Id, bool kDemand>
+__global__ void __launch_bounds__(kBlock) k_dispatch(Routing r, int hosts, int once, int32_t* counts, double* demand) {
+  const long long i = (long long)blockIdx.x * kBlock + threadIdx.x;
+  if (i >= r.tokens * r.k) return;
+  const long long t = i / r.k;
+  const int j = (int)(i - t * r.k);
+  int lo = 0, hi = r.sources + 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (r.host_begin[mid] <= t) lo = mid + 1; else hi = mid;
+  }
+  const int s = lo - 1;
+  if (s < 0 || s >= r.sources) return;
+  if constexpr (kDemand) {
+    const int h = host_of<Id>(r, t, j, hosts);
+    if (h < 0) return;
+    if (once)
+      for (int i = 0; i < j; ++i)
+        if (host_of<Id>(r, t, i, hosts) == h) return;
+    unsafeAtomicAdd(demand + (size_t)h * r.sources + s, 1.0);
+  } else {
+    const Id e = ((const Id*)r.choices)[t * r.stride + j];
+    if (e >= 0 && e < r.experts) atomicAdd(counts + (size_t)s * r.experts + e, 1);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// balance loss
+// ---------------------------------------------------------------------------------------
+//
+// A row of logits lies in kLanes lanes, kValues numbers in each, and a wave has 64 / kLanes rows at a time: maximum and sum
+// are taken in the lane first and between the lanes of a row then.  A lane keeps the sums of its experts' probabilities
+// for as long as the source stays the same; what the waves of a workgroup have for it is added up once a piece.
+
+struct Balance {
+  Routing r;
+  const void* logits;
+  long long logits_stride, per;
+  const double* cost;
+  int hosts;
+  // places of pieces (a2a_dispatch_plan.h)
+  float* sums;
+  int32_t* counts;
+  int32_t* rows;
+  // the call's
+  double* terms;
+  float* out_loss;
+  int32_t* out_counts;
+  float* out_sums;
+  int32_t* out_rows;
+  // gradient
+  const int32_t* in_counts;
+  const int32_t* in_rows;
+  const float* upstream;
+  void* grad;
+  long long grad_stride;
+};
+
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float x) {
+  const int i = __float_as_int(x);
+  return __int_as_float(__builtin_amdgcn_update_dpp(i, i, kCtrl, 0xf, 0xf, false));
+}
+
+// f over the kLanes lanes of a row, in all of them.  Lanes of a quad, then of halves and wholes of 16 (mirrored: the quads
+// agree by then), then across.
+template <int kLanes, typename F>
+__device__ __forceinline__ float over_lanes(float x, F f) {
+  if constexpr (kLanes > 1) x = f(x, dpp<0xb1>(x));
+  if constexpr (kLanes > 2) x = f(x, dpp<0x4e>(x));
+  if constexpr (kLanes > 4) x = f(x, dpp<0x141>(x));
+  if constexpr (kLanes > 8) x = f(x, dpp<0x140>(x));
+  if constexpr (kLanes > 16) x = f(x, __shfl_xor(x, 16, kWave));
+  if constexpr (kLanes > 32) x = f(x, __shfl_xor(x, 32, kWave));
+  return x;
+}
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__bf16 x) { return (float)x; }
+__device__ __forceinline__ float to_float(_Float16 x) { return (float)x; }
+
+// The numbers of a row that a lane has.  Pieces of 16 bytes (kWide: rows begin at multiples of 16 bytes) or one number at
+// a time, neighbours in neighbouring lanes.
+template <typename T, bool kWide, int kLanes, int kValues>
+struct Row {
+  static constexpr int kPiece = kWide ? 16 / (int)sizeof(T) : 1;
+  static constexpr int kPieces = kValues / kPiece;
+  typedef T Piece __attribute__((ext_vector_type(kPiece)));
+  Piece p[kPieces];
+
+  static __device__ __forceinline__ int expert(int lane, int i) {  // of a lane's number i
+    return (i / kPiece * kLanes + lane) * kPiece + i % kPiece;
+  }
+  __device__ __forceinline__ void load(const T* __restrict__ row, int lane, int experts) {
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+      const int e = expert(lane, q * kPiece);
+      if (e + kPiece <= experts) {
+        p[q] = *reinterpret_cast<const Piece*>(row + e);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) p[q][j] = e + j < experts ? row[e + j] : (T)-INFINITY;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* __restrict__ row, int lane, int experts) const {
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+      const int e = expert(lane, q * kPiece);
+      if (e + kPiece <= experts) {
+        *reinterpret_cast<Piece*>(row + e) = p[q];
+      } else {
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j)
+          if (e + j < experts) row[e + j] = p[q][j];
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int i) const { return to_float(p[i / kPiece][i % kPiece]); }
+  __device__ __forceinline__ void set(int i, float x) { p[i / kPiece][i % kPiece] = (T)x; }
+
+  // x[i] = exp(z_i - maximum); returns their sum over the row, 0 for a row of -infinity alone.  (exp2(z log2(e) - maximum log2(e))
+  // by one multiply-add would be off by the rounding of the second product, which for a row of a mask's lowest values is
+  // past any exponent.)
+  __device__ __forceinline__ float exponentials(float (&x)[kValues]) const {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) top = fmaxf(top, get(i));
+    top = over_lanes<kLanes>(top, [](float a, float b) { return fmaxf(a, b); });
+    constexpr float kLog2e = 1.44269504088896340736f;
+    top = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) {
+      x[i] = __builtin_amdgcn_exp2f((get(i) - top) * kLog2e);
+      sum += x[i];
+    }
+    return over_lanes<kLanes>(sum, [](float a, float b) { return a + b; });
+  }
+};
+
+// The pieces of workgroup b, in order: f(source, first token, token behind the last).
+template <typename F>
+__device__ __forceinline__ void for_pieces(const Routing& r, long long per, F&& f) {
+  long long t = (long long)blockIdx.x * per;
+  const long long end = min(t + per, r.tokens);
+  while (t < end) {
+    const int n = begun(r.host_begin, r.sources + 1, t);
+    if (n > r.sources) break;                            // behind the last source's tokens
+    long long next = min(end, (long long)r.host_begin[n]);
+    next = max(next, t + 1);
+    if (n > 0) f(n - 1, t, next);
+    t = next;
+  }
+}
+
+template <typename T, bool kWide, int kLanes, int kValues, typename Id>
+__global__ void __launch_bounds__(kBalanceThreads) k_balance_rows(Balance b) {
+  using R = Row<T, kWide, kLanes, kValues>;
+  constexpr int kWaves = kBalanceThreads / kWave, kRows = kWave / kLanes;
+  extern __shared__ float lds[];  // [kWaves][experts] sums, int [experts] counts, int [kWaves] rows
+  const int X = b.r.experts, k = b.r.k;
+  int* const counts = (int*)(lds + kWaves * X);
+  int* const rows = counts + X;
+  const int wave = threadIdx.x / kWave, lane = lane_id() % kLanes, slot = lane_id() / kLanes;
+  for_pieces(b.r, b.per, [&](int s, long long t0, long long t1) {
+    for (int e = threadIdx.x; e < X; e += kBalanceThreads) counts[e] = 0;
+    __syncthreads();
+    float acc[kValues] = {};
+    int mine = 0;
+    for (long long t = t0 + wave * kRows + slot; t - slot < t1; t += kWaves * kRows) {
+      float x[kValues], inv = 0.0f;
+      bool token = false;
+      if (t < t1) {
+        R row;
+        row.load((const T*)b.logits + t * b.logits_stride, lane, X);
+        const float sum = row.exponentials(x);
+        token = sum != 0.0f;
+        inv = token ? 1.0f / sum : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kValues; ++i) acc[i] = __builtin_fmaf(x[i], inv, acc[i]);
+        if (token) {
+          mine += lane == 0;
+          for (int j = lane; j < k; j += kLanes) {
+            const Id e = ((const Id*)b.r.choices)[t * b.r.stride + j];
+            if (e >= 0 && e < X) atomicAdd(&counts[e], 1);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) {
+#pragma unroll
+      for (int m = kLanes; m < kWave; m *= 2) acc[i] += __shfl_xor(acc[i], m, kWave);
+      const int e = R::expert(lane, i);
+      if (slot == 0 && e < X) lds[wave * X + e] = acc[i];
+    }
+#pragma unroll
+    for (int m = kLanes; m < kWave; m *= 2) mine += __shfl_xor(mine, m, kWave);
+    if (lane_id() == 0) rows[wave] = mine;
+    __syncthreads();
+    const size_t place = (size_t)blockIdx.x + s;
+    for (int e = threadIdx.x; e < X; e += kBalanceThreads) {
+      float sum = lds[e];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) sum += lds[w * X + e];
+      b.sums[place * X + e] = sum;
+      b.counts[place * X + e] = counts[e];
+    }
+    if (threadIdx.x == 0) {
+      int n = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) n += rows[w];
+      b.rows[place] = n;
+    }
+    __syncthreads();
+  });
+}
+
+__device__ __forceinline__ double weight_of(const Balance& b, int s, int e) {
+  if (!b.cost) return 1.0;
+  const int h = b.r.expert_host ? b.r.expert_host[e] : e;
+  return h >= 0 && h < b.hosts ? b.cost[(size_t)s * b.hosts + h] : 0.0;
+}
+
+// Sum over the workgroup, in thread 0, in a fixed order.
+__device__ __forceinline__ double block_sum(double x, double* lds) {
+#pragma unroll
+  for (int m = 1; m < kWave; m *= 2) x += __shfl_xor(x, m, kWave);
+  if (lane_id() == 0) lds[threadIdx.x / kWave] = x;
+  __syncthreads();
+  double sum = 0.0;
+  if (threadIdx.x == 0)
+    for (int w = 0; w < (int)blockDim.x / kWave; ++w) sum += lds[w];
+  __syncthreads();
+  return sum;
+}
+
+// A source's pieces, added up in the order of its tokens, and its term of the loss: double precision from here on.
+static __global__ void __launch_bounds__(kBalanceThreads) k_balance_sources(Balance b) {
+  __shared__ double lds[kBalanceThreads / kWave];
+  const int s = blockIdx.x, X = b.r.experts;
+  const long long first = min(max((long long)b.r.host_begin[s], 0ll), b.r.tokens);
+  const long long behind = min((long long)b.r.host_begin[s + 1], b.r.tokens);
+  const long long b0 = first / b.per, b1 = behind > first ? (behind - 1) / b.per : b0 - 1;
+  int rows = 0;
+  for (long long g = b0; g <= b1; ++g) rows += b.rows[g + s];
+  double term = 0.0;
+  for (int e = threadIdx.x; e < X; e += kBalanceThreads) {
+    double sum = 0.0;
+    int count = 0;
+    for (long long g = b0; g <= b1; ++g) {
+      sum += b.sums[(g + s) * X + e];
+      count += b.counts[(g + s) * X + e];
+    }
+    b.out_sums[(size_t)s * X + e] = (float)sum;
+    b.out_counts[(size_t)s * X + e] = count;
+    if (rows > 0) term += weight_of(b, s, e) * count * sum;
+  }
+  term = block_sum(term, lds);
+  if (threadIdx.x == 0) {
+    b.out_rows[s] = rows;
+    b.terms[s] = rows > 0 ? term / rows : 0.0;
+  }
+}
+
+// The loss from the sources' terms.
+static __global__ void __launch_bounds__(kBalanceThreads) k_balance_loss(Balance b) {
+  __shared__ double lds[kBalanceThreads / kWave];
+  double sum = 0.0, rows = 0.0;
+  for (int s = threadIdx.x; s < b.r.sources; s += kBalanceThreads) {
+    sum += b.terms[s];
+    rows += b.out_rows[s];
+  }
+  sum = block_sum(sum, lds);
+  rows = block_sum(rows, lds);
+  if (threadIdx.x == 0) b.out_loss[0] = rows > 0.0 ? (float)(sum * b.r.experts / (b.r.k * rows)) : 0.0f;
+}
+
+template <typename T, bool kWide, int kLanes, int kValues>
+__global__ void __launch_bounds__(kBalanceThreads) k_balance_grad(Balance b) {
+  using R = Row<T, kWide, kLanes, kValues>;
+  constexpr int kWaves = kBalanceThreads / kWave, kRows = kWave / kLanes;
+  extern __shared__ double lds64[];  // [kWaves] doubles, float [experts]
+  float* const coef = (float*)(lds64 + kWaves + 1);
+  const int X = b.r.experts;
+  const int wave = threadIdx.x / kWave, lane = lane_id() % kLanes, slot = lane_id() / kLanes;
+  double n = 0.0;
+  for (int s = threadIdx.x; s < b.r.sources; s += kBalanceThreads) n += b.in_rows[s];
+  n = block_sum(n, lds64);
+  if (threadIdx.x == 0) lds64[kWaves] = n > 0.0 ? (b.upstream ? (double)b.upstream[0] : 1.0) * X / (b.r.k * n) : 0.0;
+  __syncthreads();
+  const double scale = lds64[kWaves];
+  for_pieces(b.r, b.per, [&](int s, long long t0, long long t1) {
+    const double of_source = scale / max(b.in_rows[s], 1);
+    for (int e = threadIdx.x; e < X; e += kBalanceThreads)
+      coef[e] = (float)(of_source * weight_of(b, s, e) * b.in_counts[(size_t)s * X + e]);
+    __syncthreads();
+    float c[kValues];
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) {
+      const int e = R::expert(lane, i);
+      c[i] = e < X ? coef[e] : 0.0f;
+    }
+    for (long long t = t0 + wave * kRows + slot; t < t1; t += kWaves * kRows) {
+      float x[kValues];
+      R row;
+      row.load((const T*)b.logits + t * b.logits_stride, lane, X);
+      const float sum = row.exponentials(x);
+      float dot = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) dot = __builtin_fmaf(x[i], c[i], dot);
+      dot = over_lanes<kLanes>(dot, [](float a, float b) { return a + b; });
+      const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+      dot *= inv;
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) row.set(i, x[i] * inv * (c[i] - dot));
+      row.store((T*)b.grad + t * b.grad_stride, lane, X);
+    }
+    __syncthreads();
+  });
+}
+
+}  // namespace a2a_dev

@@ -1,0 +1,89 @@
+// What the dispatch functions accept and how their calls are cut up: plain host arithmetic, no HIP, so that it can be
+// checked over its whole range without a device.
+#pragma once
+
+#include <algorithm>
+#include <cstddef>
+#include <cstdint>
+
+#include "a2a_topo.h"
+
+namespace a2a_dev {
+
+constexpr int kMostChoices = 64;
+
+inline size_t type_bytes(int type) {
+  switch (type) {
+    case A2A_F32: case A2A_I32: return 4;
+    case A2A_BF16: case A2A_F16: return 2;
+    case A2A_I64: return 8;
+    default: return 0;
+  }
+}
+
+inline bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// rows x stride numbers of `bytes` each stay within an address space
+inline bool spans(int64_t rows, int64_t stride, size_t bytes) {
+  return stride <= 0 || rows <= (int64_t)((uint64_t)INT64_MAX / bytes) / stride;
+}
+
+// Arguments that all dispatch functions have.  choices: whether they are read.
+inline int check_routing(int32_t src_count, const a2a_routing* r, bool choices) {
+  if (src_count < 0 || !r || r->tokens < 0 || r->experts < 1 || r->reserved != 0) return A2A_ERR_INVALID_ARG;
+  if (r->choices_per_token < 1 || r->choices_per_token > kMostChoices) return A2A_ERR_INVALID_ARG;
+  if (r->tokens > (int64_t)INT32_MAX / r->choices_per_token) return A2A_ERR_NOT_IMPLEMENTED;  // counts are 32 bits
+  if (src_count > 0 && (!r->host_begin || !aligned_to(r->host_begin, 8))) return A2A_ERR_INVALID_ARG;
+  if (!aligned_to(r->expert_host, 4)) return A2A_ERR_INVALID_ARG;
+  if (!choices) return A2A_OK;
+  if (r->choices_type != A2A_I32 && r->choices_type != A2A_I64) return A2A_ERR_INVALID_ARG;
+  if (r->choices_stride < r->choices_per_token || !spans(r->tokens, r->choices_stride, 8)) return A2A_ERR_INVALID_ARG;
+  if (src_count > 0 && r->tokens > 0 && (!r->choices || !aligned_to(r->choices, type_bytes(r->choices_type)))) return A2A_ERR_INVALID_ARG;
+  return A2A_OK;
+}
+
+// A matrix of logits (or of their gradients) for the routing's tokens.
+inline int check_logits(const a2a_routing* r, const void* logits, int type, int64_t stride) {
+  if (type != A2A_F32 && type != A2A_BF16 && type != A2A_F16) return A2A_ERR_INVALID_ARG;
+  if (r->experts > A2A_MOST_EXPERTS) return A2A_ERR_NOT_IMPLEMENTED;
+  if (stride < r->experts || !spans(r->tokens, stride, 4)) return A2A_ERR_INVALID_ARG;
+  if (r->tokens > 0 && (!logits || !aligned_to(logits, type_bytes(type)))) return A2A_ERR_INVALID_ARG;
+  return A2A_OK;
+}
+
+// Passes over logits: a workgroup has `per` consecutive tokens, of as many sources as they belong to.  The tokens of
+// workgroup b that belong to source s are its piece (b, s).  Pieces follow each other, and from one to the next b or s
+// grows, so b + s numbers them: the sums of a piece have place b + s of the workspace, and those of source s are the
+// places b + s of the workgroups b that its tokens fall into.
+constexpr int kBalanceThreads = 256;
+struct BalanceCut {
+  int64_t per = 0;     // tokens a workgroup
+  int64_t groups = 0;  // workgroups
+};
+inline BalanceCut balance_cut(int64_t tokens) {
+  BalanceCut c;
+  c.per = std::max<int64_t>(64, (tokens + 2047) / 2048);
+  c.groups = (tokens + c.per - 1) / c.per;
+  return c;
+}
+struct BalanceLayout {
+  size_t sums = 0, counts = 0, rows = 0, terms = 0, total = 0;
+};
+inline BalanceLayout balance_layout(int64_t src_count, int64_t tokens, int64_t experts) {
+  const int64_t places = balance_cut(tokens).groups + src_count;
+  BalanceLayout l;
+  size_t off = 0;
+  const auto part = [&off](size_t bytes) {
+    const size_t at = off;
+    off += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  l.sums = part((size_t)places * experts * 4);
+  l.counts = part((size_t)places * experts * 4);
+  l.rows = part((size_t)places * 4);
+  l.terms = part((size_t)src_count * 8);
+  l.total = off;
+  return l;
+}
+
+}  // namespace a2a_dev

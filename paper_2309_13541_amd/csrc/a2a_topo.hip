@@ -33,6 +33,8 @@
 #include <new>
 #include <vector>
 
+#include "a2a_cost_kernels.h"
+#include "a2a_dispatch_kernels.h"
 #include "a2a_kernels.h"
 #include "a2a_launch.h"
 #include "a2a_sssp_kernels.h"
@@ -230,7 +232,7 @@ enum {
   PROF_INIT = A2A_K_INIT, PROF_BFS = A2A_K_BFS, PROF_OFFSETS = A2A_K_OFFSETS, PROF_FWD = A2A_K_FWD_ROWS,
   PROF_FWD_FEW = A2A_K_FWD_FEW, PROF_FWD_SPREAD = A2A_K_FWD_SPREAD, PROF_BWD = A2A_K_BWD_ROWS,
   PROF_BWD_FEW = A2A_K_BWD_FEW, PROF_BWD_SPREAD = A2A_K_BWD_SPREAD, PROF_REDUCE = A2A_K_REDUCE, PROF_EXTRACT = A2A_K_EXTRACT,
-  PROF_SEARCH = A2A_K_SEARCH, PROF_SOURCES = A2A_K_SOURCES,
+  PROF_SEARCH = A2A_K_SEARCH, PROF_SOURCES = A2A_K_SOURCES, PROF_TOKENS = A2A_K_TOKENS,
   PROF_CLASSES = A2A_K_COUNT
 };
 
@@ -1202,6 +1204,125 @@ int small_sssp(const a2a_topo* t, int32_t src_begin, int32_t src_count, int32_t 
   return A2A_OK;
 }
 
+size_t cost_workspace_bytes(const a2a_topo*) { return 256; }
+
+Routing routing_of(const a2a_routing* r, int32_t src_count) {
+  return Routing{r->choices, r->host_begin, r->expert_host, (long long)r->tokens, (long long)r->choices_stride,
+                 r->choices_per_token, r->experts, src_count};
+}
+
+// counts or demand: the other is null
+int dispatch(const a2a_topo* t, int32_t src_count, const a2a_routing* routing, int once, int32_t* counts, double* demand,
+             hipStream_t st) {
+  const Use use(t, st);
+  const Routing r = routing_of(routing, src_count);
+  ProfScope ps(t, PROF_TOKENS, st);
+  if (counts) {
+    const size_t cells = (size_t)src_count * r.experts;
+    k_fill<<<(unsigned)std::min<size_t>((cells + kBlock - 1) / kBlock, 16384), kBlock, 0, st>>>(counts, cells);
+  } else {
+    HIP_TRY(zero_async(demand, (size_t)t->N * src_count * 8, st));
+  }
+  const unsigned blocks = (unsigned)((r.tokens * r.k + kBlock - 1) / kBlock);
+  if (blocks > 0) {
+    const bool wide = routing->choices_type == A2A_I64;
+    const auto launch = [&](auto kernel) { kernel<<<blocks, kBlock, 0, st>>>(r, t->N, once, counts, demand); };
+    if (counts)
+      wide ? launch(k_dispatch<int64_t, false>) : launch(k_dispatch<int32_t, false>);
+    else
+      wide ? launch(k_dispatch<int64_t, true>) : launch(k_dispatch<int32_t, true>);
+  }
+  HIP_TRY(hipGetLastError());
+  return A2A_OK;
+}
+
+// f(kLanes, kValues), constants, that hold `experts` numbers (a2a_dispatch_kernels.h).
+template <typename F>
+void by_row(int experts, bool wide, F&& f) {
+  const auto call = [&](auto lanes, auto values) { f(lanes, values); };
+  using std::integral_constant;
+  if (!wide) {
+    if (experts <= 16 * 8) call(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+    else if (experts <= 16 * 32) call(integral_constant<int, 16>{}, integral_constant<int, 32>{});
+    else call(integral_constant<int, 64>{}, integral_constant<int, 64>{});
+    return;
+  }
+  if (experts <= 8) call(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+  else if (experts <= 16) call(integral_constant<int, 2>{}, integral_constant<int, 8>{});
+  else if (experts <= 32) call(integral_constant<int, 4>{}, integral_constant<int, 8>{});
+  else if (experts <= 64) call(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+  else if (experts <= 128) call(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+  else if (experts <= 256) call(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+  else if (experts <= 512) call(integral_constant<int, 16>{}, integral_constant<int, 32>{});
+  else if (experts <= 1024) call(integral_constant<int, 16>{}, integral_constant<int, 64>{});
+  else call(integral_constant<int, 64>{}, integral_constant<int, 64>{});
+}
+
+// f(x), x a number of the type
+template <typename F>
+void by_float(int type, F&& f) {
+  switch (type) {
+    case A2A_F32: f(float{}); break;
+    case A2A_BF16: f(__bf16{}); break;
+    default: f(_Float16{}); break;
+  }
+}
+
+bool rows_of_pieces(const void* p, int64_t stride, size_t bytes) { return aligned_to(p, 16) && stride * bytes % 16 == 0; }
+
+int balance_loss(const a2a_topo* t, const a2a_routing* routing, int type, Balance& b, hipStream_t st) {
+  const Use use(t, st);
+  ProfScope ps(t, PROF_TOKENS, st);
+  const BalanceCut cut = balance_cut(b.r.tokens);
+  b.per = cut.per;
+  if (cut.groups > 0 && b.r.sources > 0) {
+    const bool wide = rows_of_pieces(b.logits, b.logits_stride, type_bytes(type));
+    const size_t lds = ((size_t)(kBalanceThreads / kWave + 1) * b.r.experts + kBalanceThreads / kWave) * 4;
+    by_float(type, [&](auto x) {
+      using T = decltype(x);
+      by_row(b.r.experts, wide, [&](auto lanes, auto values) {
+        constexpr int L = decltype(lanes)::value, V = decltype(values)::value;
+        const auto launch = [&](auto kernel) { kernel<<<(unsigned)cut.groups, kBalanceThreads, lds, st>>>(b); };
+        if (routing->choices_type == A2A_I64)
+          wide ? launch(k_balance_rows<T, true, L, V, int64_t>) : launch(k_balance_rows<T, false, L, V, int64_t>);
+        else
+          wide ? launch(k_balance_rows<T, true, L, V, int32_t>) : launch(k_balance_rows<T, false, L, V, int32_t>);
+      });
+    });
+  }
+  if (b.r.sources > 0) k_balance_sources<<<(unsigned)b.r.sources, kBalanceThreads, 0, st>>>(b);
+  k_balance_loss<<<1, kBalanceThreads, 0, st>>>(b);
+  HIP_TRY(hipGetLastError());
+  return A2A_OK;
+}
+
+int balance_grad(const a2a_topo* t, int type, Balance& b, hipStream_t st) {
+  const Use use(t, st);
+  ProfScope ps(t, PROF_TOKENS, st);
+  const BalanceCut cut = balance_cut(b.r.tokens);
+  b.per = cut.per;
+  if (cut.groups == 0 || b.r.sources == 0) return A2A_OK;
+  const size_t bytes = type_bytes(type);
+  const bool wide = rows_of_pieces(b.logits, b.logits_stride, bytes) && rows_of_pieces(b.grad, b.grad_stride, bytes);
+  const size_t lds = (kBalanceThreads / kWave + 1) * 8 + (size_t)b.r.experts * 4;
+  by_float(type, [&](auto x) {
+    using T = decltype(x);
+    by_row(b.r.experts, wide, [&](auto lanes, auto values) {
+      constexpr int L = decltype(lanes)::value, V = decltype(values)::value;
+      const auto launch = [&](auto kernel) { kernel<<<(unsigned)cut.groups, kBalanceThreads, lds, st>>>(b); };
+      wide ? launch(k_balance_grad<T, true, L, V>) : launch(k_balance_grad<T, false, L, V>);
+    });
+  });
+  HIP_TRY(hipGetLastError());
+  return A2A_OK;
+}
+
+// The handle's device is the current one.
+bool on_device(const a2a_topo* t) {
+  int device = -1;
+  return hipGetDevice(&device) == hipSuccess && device == t->mem.device;
+}
+
 int check_common(const a2a_topo* t, int32_t src_begin, int32_t src_count, void* ws) {
   if (!t || src_begin < 0 || src_count < 0 || (int64_t)src_begin + src_count > t->N) return A2A_ERR_INVALID_ARG;
   if (src_count > 0 && (!ws || ((uintptr_t)ws & 255u))) return A2A_ERR_INVALID_ARG;
@@ -1348,6 +1469,7 @@ int a2a_topo_info(const a2a_topo* t, int32_t* N, int64_t* E, int32_t* dmax, int3
 size_t a2a_workspace_bytes(const a2a_topo* t, int32_t src_count, int flags) {
   if (!t || src_count < 0 || (size_t)src_count > align_up((size_t)t->N, 64)) return 0;
   if (src_count == 0) return 256;
+  if (flags & A2A_WS_COSTS) return cost_workspace_bytes(t);
   const bool minimal = (flags & A2A_WS_MINIMAL) != 0;
   const Layout L = make_layout(t, src_count, flags & 0xff, 0, true, minimal);
   return minimal || !(flags & A2A_WS_LOADS) || !t->small_loads ? L.total : std::max(L.total, small_loads_bytes(t, src_count));
@@ -1611,6 +1733,104 @@ int a2a_sssp_loads(const a2a_topo* t, int32_t src_begin, int32_t src_count, int3
                              nullptr, (long long*)flags);
   HIP_TRY(hipGetLastError());
   return A2A_OK;
+}
+
+int a2a_path_costs(const a2a_topo* t, int32_t src_begin, int32_t src_count, const int32_t* dist, const double* sigma,
+                   const double* link_cost, double* cost, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_common(t, src_begin, src_count, workspace);
+  if (rc != A2A_OK) return rc;
+  if (src_count == 0) return A2A_OK;
+  if (!dist || !sigma || !cost || !aligned_to(dist, 4) || !aligned_to(sigma, 8) || !aligned_to(cost, 8) || !aligned_to(link_cost, 8) ||
+      !on_device(t))
+    return A2A_ERR_INVALID_ARG;
+  if (workspace_bytes < cost_workspace_bytes(t)) return A2A_ERR_WORKSPACE_TOO_SMALL;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const Use use(t, st);
+  ProfScope ps(t, PROF_SOURCES, st);
+  const CostView c{t->d_in_ptr, t->d_in_col, t->d_in_link, dist, sigma, link_cost, cost, t->N, src_count, t->level_bound};
+  k_path_costs<<<(unsigned)std::min(src_count, 65535), kCostThreads, 0, st>>>(c);
+  HIP_TRY(hipGetLastError());
+  return A2A_OK;
+}
+
+int a2a_dispatch_counts(const a2a_topo* t, int32_t src_count, const a2a_routing* routing, int32_t* counts, void* hip_stream) {
+  if (!t) return A2A_ERR_INVALID_ARG;
+  const int rc = check_routing(src_count, routing, true);
+  if (rc != A2A_OK) return rc;
+  if (src_count == 0) return A2A_OK;
+  if (!counts || !aligned_to(counts, 4) || !on_device(t)) return A2A_ERR_INVALID_ARG;
+  return dispatch(t, src_count, routing, 0, counts, nullptr, (hipStream_t)hip_stream);
+}
+
+int a2a_dispatch_demand(const a2a_topo* t, int32_t src_count, const a2a_routing* routing, int once, double* demand,
+                        void* hip_stream) {
+  if (!t) return A2A_ERR_INVALID_ARG;
+  const int rc = check_routing(src_count, routing, true);
+  if (rc != A2A_OK) return rc;
+  if (src_count > t->N || (once != 0 && once != 1)) return A2A_ERR_INVALID_ARG;
+  if (src_count == 0) return A2A_OK;
+  if (!demand || !aligned_to(demand, 8) || !on_device(t)) return A2A_ERR_INVALID_ARG;
+  return dispatch(t, src_count, routing, once, nullptr, demand, (hipStream_t)hip_stream);
+}
+
+size_t a2a_balance_workspace_bytes(const a2a_topo* t, int32_t src_count, int64_t tokens, int32_t experts) {
+  if (!t || src_count < 0 || tokens < 0 || tokens > INT32_MAX || experts < 1 || experts > A2A_MOST_EXPERTS) return 0;
+  return balance_layout(src_count, tokens, experts).total;
+}
+
+int a2a_balance_loss(const a2a_topo* t, int32_t src_count, const a2a_routing* routing, const void* logits, int logits_type,
+                     int64_t logits_stride, const double* cost, float* loss, int32_t* counts, float* prob_sums, int32_t* rows,
+                     void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!t) return A2A_ERR_INVALID_ARG;
+  int rc = check_routing(src_count, routing, true);
+  if (rc == A2A_OK) rc = check_logits(routing, logits, logits_type, logits_stride);
+  if (rc != A2A_OK) return rc;
+  if (!loss || !aligned_to(loss, 4) || !aligned_to(cost, 8) || !on_device(t)) return A2A_ERR_INVALID_ARG;
+  if (src_count > 0 && (!counts || !aligned_to(counts, 4) || !prob_sums || !aligned_to(prob_sums, 4) || !rows || !aligned_to(rows, 4) ||
+                        !workspace || !aligned_to(workspace, 256)))
+    return A2A_ERR_INVALID_ARG;
+  const BalanceLayout l = balance_layout(src_count, routing->tokens, routing->experts);
+  if (src_count > 0 && workspace_bytes < l.total) return A2A_ERR_WORKSPACE_TOO_SMALL;
+  char* const ws = (char*)workspace;
+  Balance b{};
+  b.r = routing_of(routing, src_count);
+  b.logits = logits;
+  b.logits_stride = logits_stride;
+  b.cost = cost;
+  b.hosts = t->N;
+  b.sums = (float*)(ws + l.sums);
+  b.counts = (int32_t*)(ws + l.counts);
+  b.rows = (int32_t*)(ws + l.rows);
+  b.terms = (double*)(ws + l.terms);
+  b.out_loss = loss;
+  b.out_counts = counts;
+  b.out_sums = prob_sums;
+  b.out_rows = rows;
+  return balance_loss(t, routing, logits_type, b, (hipStream_t)hip_stream);
+}
+
+int a2a_balance_loss_grad(const a2a_topo* t, int32_t src_count, const a2a_routing* routing, const void* logits, int logits_type,
+                          int64_t logits_stride, const double* cost, const int32_t* counts, const int32_t* rows,
+                          const float* upstream, void* grad, int64_t grad_stride, void* hip_stream) {
+  if (!t) return A2A_ERR_INVALID_ARG;
+  int rc = check_routing(src_count, routing, false);
+  if (rc == A2A_OK) rc = check_logits(routing, logits, logits_type, logits_stride);
+  if (rc == A2A_OK) rc = check_logits(routing, grad, logits_type, grad_stride);
+  if (rc != A2A_OK) return rc;
+  if (!aligned_to(cost, 8) || !aligned_to(upstream, 4) || !on_device(t)) return A2A_ERR_INVALID_ARG;
+  if (src_count > 0 && (!counts || !aligned_to(counts, 4) || !rows || !aligned_to(rows, 4))) return A2A_ERR_INVALID_ARG;
+  Balance b{};
+  b.r = routing_of(routing, src_count);
+  b.logits = logits;
+  b.logits_stride = logits_stride;
+  b.cost = cost;
+  b.hosts = t->N;
+  b.in_counts = counts;
+  b.in_rows = rows;
+  b.upstream = upstream;
+  b.grad = grad;
+  b.grad_stride = grad_stride;
+  return balance_grad(t, logits_type, b, (hipStream_t)hip_stream);
 }
 
 int a2a_schedule_bound(const a2a_topo* t, const double* load, int64_t sum_dist, int64_t flags,
