@@ -1,25 +1,256 @@
 // Device code of a2a_path_costs.
+//
+// A last link u -> v of a shortest path to v carries sigma(u) of its sigma(v) paths, so with C(v) = sigma(v) cost(v), the
+// costs of all shortest paths to v together,
+//   C(v) = B(v) + sum_u C(u),  B(v) = sum_u sigma(u) link_cost(u -> v),
+// over the links u -> v with D(u) = D(v) - 1.  B and which links these are need no cost of any other node: all nodes at
+// once.  The sums need the level before: level by level.  One division at the end.
 #pragma once
 
-#include "a2a_kernels.h"
+#include "a2a_cost_plan.h"
+#include "a2a_small_kernels.h"
 
 namespace a2a_dev {
 
 struct CostView {
   const int32_t *in_ptr, *in_col, *in_link;
+  const uint32_t* in;  // link table (SmallView), or null
   const int32_t* dist;
   const double* sigma;
   const double* link_cost;
+  double* prices;   // of the places of the link table, if there are link costs
+  uint32_t* lists;  // [workgroups][N]
   double* cost;
-  int N, sources, depth;
+  int N, sources, depth, words;
 };
 
-constexpr int kCostThreads = 1024;
+// Link costs by place of the link table.
+static __global__ void __launch_bounds__(kBlock) k_cost_prices(CostView c) {
+  const int places = 2 * c.words;
+  const int i = blockIdx.x * kBlock + threadIdx.x;
+  if (i >= c.N * places) return;
+  const int v = i / places, p = c.in_ptr[v] + (i - v * places);
+  c.prices[i] = p < c.in_ptr[v + 1] ? c.link_cost[c.in_link[p]] : 0.0;
+}
 
-// A workgroup per source.  Every last link u -> v of a shortest path to v carries sigma(u) of the sigma(v) paths:
-//   cost(v) = sum_u sigma(u) (cost(u) + link_cost(u -> v)) / sum_u sigma(u),
-// level by level, so that the costs of the level before are there.
-static __global__ void __launch_bounds__(kCostThreads) k_path_costs(CostView c) {
+// Lanes whose x, of `bits` bits, is this lane's.
+__device__ __forceinline__ uint64_t lanes_like(unsigned x, int bits) {
+  uint64_t m = ~0ull;
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t set = __ballot(x >> b & 1u);
+    m &= x >> b & 1u ? set : ~set;
+  }
+  return m;
+}
+
+// A workgroup per source, its state in LDS: an array of doubles that holds path counts, then B, then C; a level byte a
+// node; the nodes in the order of levels, with a bit for each place of the link table that is a last link.  A thread has
+// kNodes nodes for what needs no order.  Places in a level are handed out a wave at a time (an atomic addition a level and
+// wave); their order changes nothing, a node's sum is its own.
+template <int KS, int kNodes>
+__global__ void __launch_bounds__(kCostThreads) k_cost_sources(CostView c) {
+  constexpr bool kInLds = cost_list_in_lds(kNodes);
+  constexpr int kShift = kNodes < 16 ? 3 : 0;  // ids of the table are 8 x id up to kScaledNodes
+  extern __shared__ __align__(16) unsigned char cost_state[];
+  const int N = c.N, T = blockDim.x, pad = (N + 15) / 16 * 16;
+  double* const value = (double*)cost_state;
+  uint32_t* const list = kInLds ? (uint32_t*)(value + pad) : c.lists + (size_t)blockIdx.x * N;
+  int* const start = kInLds ? (int*)(value + pad) + pad : (int*)(value + pad);
+  unsigned char* const level = (unsigned char*)(start + (c.depth + 2 + 3) / 4 * 4);
+  const int bits = 32 - __builtin_clz(c.depth | 1);
+  const bool priced = c.link_cost != nullptr;
+  for (int s = blockIdx.x; s < c.sources; s += gridDim.x) {
+    const size_t row = (size_t)s * N;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));  // what a thread's nodes need is computed anew for each source: kept, it takes the registers
+    constexpr bool kKept = kNodes < 16;  // path counts in registers to the end; read again where they do not fit
+    double sigma[kNodes];
+    for (int i = tid; i < c.depth + 2; i += T) start[i] = 0;
+#pragma unroll
+    for (int i = 0; i < kNodes; ++i) {
+      const int v = tid + i * T;
+      sigma[i] = v < N ? c.sigma[row + v] : 0.0;
+    }
+    for (int v = tid; v < N; v += T) {
+      const int d = c.dist[row + v];
+      level[v] = (unsigned char)((unsigned)d <= (unsigned)c.depth ? d : kSmallUnseen);
+    }
+#pragma unroll
+    for (int i = 0; i < kNodes; ++i) {
+      const int v = tid + i * T;
+      if (v < N) value[v] = sigma[i];
+    }
+    __syncthreads();
+    const auto level_of = [&](int v) { return v < N ? (int)level[v] : kSmallUnseen; };
+    double b[kNodes];
+    uint32_t place[kNodes];  // last links above, place in its level below
+#pragma unroll
+    for (int i = 0; i < kNodes; ++i) {
+      const int v = tid + i * T;
+      const int l = level_of(v);
+      uint32_t mask = 0;
+      b[i] = 0.0;
+      if (l - 1u < (unsigned)c.depth) {
+        SmallRow<KS> r;
+        r.load(c.in, 8 * v);
+#pragma unroll
+        for (int j = 0; j < 2 * KS; ++j) mask |= (level[r.template at<0>(j) >> kShift] + 1 == l ? 1u : 0u) << j;
+        if (priced) {
+          const double2* const p = (const double2*)(c.prices + (size_t)v * (2 * KS));
+          double2 q[KS];
+#pragma unroll
+          for (int j = 0; j < KS; ++j) q[j] = p[j];
+#pragma unroll
+          for (int j = 0; j < 2 * KS; ++j)
+            if (mask >> j & 1u) b[i] = __builtin_fma(value[r.template at<0>(j) >> kShift], j & 1 ? q[j / 2].y : q[j / 2].x, b[i]);
+        } else {
+          b[i] = value[v];
+        }
+      }
+      const uint64_t like = lanes_like(l, bits) & __ballot(l != kSmallUnseen);
+      int at = 0;
+      if (l != kSmallUnseen) {
+        const int first = __builtin_ctzll(like);
+        if (lane_id() == first) at = atomicAdd(&start[l + 1], __popcll(like));
+        at = __shfl(at, first, kWave) + (int)rank_in(like);
+      }
+      place[i] = mask << 16 | (uint32_t)at;
+      __builtin_amdgcn_sched_barrier(0);  // rows of several nodes at a time do not fit the registers
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kNodes; ++i) {
+      const int v = tid + i * T;
+      if (v < N) value[v] = b[i];
+    }
+    if (tid < kWave) {  // starts from counts
+      int before = 0;
+      for (int i0 = 0; i0 < c.depth + 2; i0 += kWave) {
+        const int i = i0 + lane_id();
+        int x = i < c.depth + 2 ? start[i] : 0;
+#pragma unroll
+        for (int m = 1; m < kWave; m *= 2) {
+          const int y = __shfl_up(x, m, kWave);
+          if (lane_id() >= m) x += y;
+        }
+        x += before;
+        if (i < c.depth + 2) start[i] = x;
+        before = __shfl(x, kWave - 1, kWave);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kNodes; ++i) {
+      const int v = tid + i * T;
+      const int l = level_of(v);
+      if (l != kSmallUnseen) list[start[l] + (place[i] & 0xffffu)] = (place[i] & 0xffff0000u) | (uint32_t)(v << kShift);
+    }
+    __syncthreads();
+    const auto at = [&](uint32_t id) -> double& { return value[id >> kShift]; };
+    const auto add = [&](uint32_t w, const SmallRow<KS>& r) {
+      double x = at(w & 0xffffu);
+#pragma unroll
+      for (int j = 0; j < 2 * KS; ++j)
+        if (w >> (16 + j) & 1u) x += at(r.template at<0>(j));
+      at(w & 0xffffu) = x;
+    };
+    const auto fetch = [&](int i, uint32_t& w, SmallRow<KS>& r) {
+      w = list[i];
+      r.load(c.in, kShift ? w & 0xffffu : (w & 0xffffu) * 8);
+    };
+    // a thread's first node of a level is asked for while the level before is worked on
+    int i0 = start[1], i1 = start[2];
+    uint32_t w = 0;
+    SmallRow<KS> r;
+    if (i0 + tid < i1) fetch(i0 + tid, w, r);
+    for (int d = 1; d <= c.depth && i0 < i1; ++d) {
+      const int i2 = d < c.depth ? start[d + 2] : i1;
+      uint32_t wn = 0;
+      SmallRow<KS> rn;
+      if (i1 + tid < i2) fetch(i1 + tid, wn, rn);
+      if (i0 + tid < i1) add(w, r);
+      for (int i = i0 + tid + T; i < i1; i += T) {
+        uint32_t wx;
+        SmallRow<KS> rx;
+        fetch(i, wx, rx);
+        add(wx, rx);
+      }
+      lds_barrier();
+      i0 = i1;
+      i1 = i2;
+      w = wn;
+      r = rn;
+    }
+#pragma unroll
+    for (int i = 0; i < kNodes; ++i) {
+      const int v = tid + i * T;
+      if (v < N) c.cost[row + v] = level[v] - 1u < (unsigned)c.depth ? value[v] / (kKept ? sigma[i] : c.sigma[row + v]) : 0.0;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();
+  }
+}
+
+// A workgroup per source, every level a pass over the level bytes of all nodes in LDS; a wave without a node of the level
+// goes on.  Costs lie in LDS (kCostsInLds) or where they go.  The mean over the last links wants path counts only where
+// there are several.
+template <int KS, bool kCostsInLds>
+__global__ void __launch_bounds__(kCostThreads) k_cost_scan(CostView c) {
+  extern __shared__ __align__(16) unsigned char cost_state[];
+  const int N = c.N, pad = (N + 15) / 16 * 16;
+  unsigned char* const level = cost_state + (kCostsInLds ? 8 * pad : 0);
+  const bool priced = c.link_cost != nullptr;
+  for (int s = blockIdx.x; s < c.sources; s += gridDim.x) {
+    const size_t row = (size_t)s * N;
+    double* const value = kCostsInLds ? (double*)cost_state : c.cost + row;
+    const double* const sigma = c.sigma + row;
+    for (int v = threadIdx.x; v < N; v += kCostThreads) {
+      const int d = c.dist[row + v];
+      const int l = (unsigned)d <= (unsigned)c.depth ? d : kSmallUnseen;
+      level[v] = (unsigned char)l;
+      if (l == 0 || l == kSmallUnseen) {
+        value[v] = 0.0;
+        if (kCostsInLds) c.cost[row + v] = 0.0;
+      }
+    }
+    __syncthreads();
+    for (int l = 1; l <= c.depth; ++l) {
+      for (int v = threadIdx.x; v < N; v += kCostThreads) {
+        if (level[v] != l) continue;
+        SmallRow<KS> r;
+        r.load(c.in, 8 * v);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int j = 0; j < 2 * KS; ++j) mask |= (level[r.template at<0>(j)] + 1 == l ? 1u : 0u) << j;
+        double sum = 0.0, paths = 0.0;
+        const double* const price = c.prices + (size_t)v * (2 * KS);
+        if ((mask & (mask - 1)) == 0) {
+#pragma unroll
+          for (int j = 0; j < 2 * KS; ++j)
+            if (mask >> j & 1u) sum = value[r.template at<0>(j)] + (priced ? price[j] : 1.0);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2 * KS; ++j)
+            if (mask >> j & 1u) {
+              const uint32_t u = r.template at<0>(j);
+              const double n = sigma[u];
+              sum = __builtin_fma(n, value[u] + (priced ? price[j] : 1.0), sum);
+              paths += n;
+            }
+          sum /= paths;
+        }
+        value[v] = sum;
+        if (kCostsInLds) c.cost[row + v] = sum;
+      }
+      kCostsInLds ? lds_barrier() : __syncthreads();
+    }
+    __syncthreads();
+  }
+}
+
+// A workgroup per source, everything in memory, a level of all nodes at a time: topologies without a link table, deep
+// ones and large ones.
+static __global__ void __launch_bounds__(kCostThreads) k_cost_levels(CostView c) {
   for (int s = blockIdx.x; s < c.sources; s += gridDim.x) {
     const size_t row = (size_t)s * c.N;
     const int32_t* const dist = c.dist + row;

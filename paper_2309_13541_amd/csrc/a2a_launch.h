@@ -4,6 +4,7 @@
 
 #include <type_traits>
 
+#include "a2a_cost_kernels.h"
 #include "a2a_flow_kernels.h"
 #include "a2a_small_kernels.h"
 #include "a2a_wide_kernels.h"
@@ -47,6 +48,9 @@ void launch_strip_sources(const FlowView& fv, int workgroups, hipStream_t st);
 // fv.exact: null after launch_flow_sources.  (With demands only after that.)
 template <int KS>
 void launch_flow_links(const FlowView& fv, bool demand, hipStream_t st);
+
+template <int KS>
+void launch_cost_sources(const CostView& cv, int nodes, int workgroups, hipStream_t st);
 
 // f(KS), a constant, for a table of that many words a node.
 template <typename F>

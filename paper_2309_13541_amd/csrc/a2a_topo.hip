@@ -33,7 +33,6 @@
 #include <new>
 #include <vector>
 
-#include "a2a_cost_kernels.h"
 #include "a2a_dispatch_kernels.h"
 #include "a2a_kernels.h"
 #include "a2a_launch.h"
@@ -1204,7 +1203,29 @@ int small_sssp(const a2a_topo* t, int32_t src_begin, int32_t src_count, int32_t 
   return A2A_OK;
 }
 
-size_t cost_workspace_bytes(const a2a_topo*) { return 256; }
+size_t cost_workspace_bytes(const a2a_topo* t) { return cost_layout(t->N, t->ell_words, t->level_bound).total; }
+
+void path_costs(const a2a_topo* t, CostView& c, char* ws, hipStream_t st) {
+  const CostWay way = cost_way(t->N, t->ell_words, t->level_bound);
+  if (way == CostWay::kLevels) {
+    ProfScope ps(t, PROF_SOURCES, st);
+    k_cost_levels<<<(unsigned)std::min(c.sources, 65535), kCostThreads, 0, st>>>(c);
+    return;
+  }
+  const CostLayout l = cost_layout(t->N, t->ell_words, t->level_bound);
+  c.in = t->d_ell_in;
+  c.prices = (double*)(ws + l.prices);
+  c.lists = (uint32_t*)(ws + l.lists);
+  c.words = t->ell_words;
+  if (c.link_cost) {
+    ProfScope ps(t, PROF_OFFSETS, st);
+    k_cost_prices<<<(unsigned)((t->N * 2 * t->ell_words + kBlock - 1) / kBlock), kBlock, 0, st>>>(c);
+  }
+  const int nodes = way == CostWay::kSources ? cost_nodes(t->N, t->ell_words, t->level_bound) : way == CostWay::kScan ? 0 : -1;
+  const int workgroups = cost_list_in_lds(nodes) ? c.sources : std::min(c.sources, kCostGroups);
+  ProfScope ps(t, PROF_SOURCES, st);
+  by_words(t->ell_words, [&](auto ks) { launch_cost_sources<decltype(ks)::value>(c, nodes, workgroups, st); });
+}
 
 Routing routing_of(const a2a_routing* r, int32_t src_count) {
   return Routing{r->choices, r->host_begin, r->expert_host, (long long)r->tokens, (long long)r->choices_stride,
@@ -1746,9 +1767,18 @@ int a2a_path_costs(const a2a_topo* t, int32_t src_begin, int32_t src_count, cons
   if (workspace_bytes < cost_workspace_bytes(t)) return A2A_ERR_WORKSPACE_TOO_SMALL;
   hipStream_t st = (hipStream_t)hip_stream;
   const Use use(t, st);
-  ProfScope ps(t, PROF_SOURCES, st);
-  const CostView c{t->d_in_ptr, t->d_in_col, t->d_in_link, dist, sigma, link_cost, cost, t->N, src_count, t->level_bound};
-  k_path_costs<<<(unsigned)std::min(src_count, 65535), kCostThreads, 0, st>>>(c);
+  CostView c{};
+  c.in_ptr = t->d_in_ptr;
+  c.in_col = t->d_in_col;
+  c.in_link = t->d_in_link;
+  c.dist = dist;
+  c.sigma = sigma;
+  c.link_cost = link_cost;
+  c.cost = cost;
+  c.N = t->N;
+  c.sources = src_count;
+  c.depth = t->level_bound;
+  path_costs(t, c, (char*)workspace, st);
   HIP_TRY(hipGetLastError());
   return A2A_OK;
 }

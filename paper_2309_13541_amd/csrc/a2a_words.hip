@@ -180,6 +180,19 @@ void launch_flow_links(const FlowView& fv, bool demand, hipStream_t st) {
     demand ? launch(k_flow_links<KS, false, true>, kNodes) : launch(k_flow_links<KS, false, false>, kNodes);
 }
 
+template <int KS>
+void launch_cost_sources(const CostView& cv, int nodes, int workgroups, hipStream_t st) {
+  const auto launch = [&](auto kernel) { kernel<<<workgroups, cost_threads(cv.N, nodes), cost_lds(cv.N, nodes, cv.depth), st>>>(cv); };
+  const auto scan = [&](auto kernel, bool costs) { kernel<<<workgroups, kCostThreads, cost_scan_lds(cv.N, costs), st>>>(cv); };
+  switch (nodes) {
+    case 0: return scan(k_cost_scan<KS, true>, true);
+    case -1: return scan(k_cost_scan<KS, false>, false);
+    case 2: return launch(k_cost_sources<KS, 2>);
+    case 8: return launch(k_cost_sources<KS, 8>);
+    default: return launch(k_cost_sources<KS, 16>);
+  }
+}
+
 template void launch_small_loads<A2A_WORDS>(const SmallPlan&, bool, int, hipStream_t);
 template void launch_node_loads<A2A_WORDS>(const SmallPlan&, bool, int, hipStream_t);
 template void launch_small_outputs<A2A_WORDS>(const SmallPlan&, const SmallOut&, int, hipStream_t);
@@ -193,5 +206,6 @@ template void launch_wide_sigma<A2A_WORDS>(const WideSigma&, int, hipStream_t);
 template void launch_flow_sources<A2A_WORDS>(const FlowView&, bool, int, hipStream_t);
 template void launch_strip_sources<A2A_WORDS>(const FlowView&, int, hipStream_t);
 template void launch_flow_links<A2A_WORDS>(const FlowView&, bool, hipStream_t);
+template void launch_cost_sources<A2A_WORDS>(const CostView&, int, int, hipStream_t);
 
 }  // namespace a2a_dev
