@@ -161,7 +161,7 @@ def _run(cmd, verbose: bool) -> None:
 
 def load_library():
     """Load liba2a_topo.so; raises if it has not been built (there is no fallback path)."""
-    global _lib
+    global _lib, _torch
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB):
@@ -171,7 +171,9 @@ def load_library():
     # PyTorch ships its own HIP runtime (same soname as the system one).  It has to be in the
     # process first, so that this library binds to the runtime that owns torch's tensors and
     # streams instead of bringing in a second one.
-    import torch  # noqa: F401
+    import torch
+    _torch = torch
+    _type_codes.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int32: 3, torch.int64: 4})
     lib = ctypes.CDLL(_LIB)
     vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     lib.a2a_topo_create.restype = ctypes.c_int
@@ -244,53 +246,47 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-# a2a_type of a torch type, by its name (torch is imported when the library is loaded)
-_TYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2, "torch.int32": 3, "torch.int64": 4}
-_type_codes = {}
-
-
-def _type_code(dtype) -> int:
-    code = _type_codes.get(dtype)
-    if code is None:
-        code = _type_codes[dtype] = _TYPES.get(str(dtype), -1)
-    return code
+_torch = None    # the module, once the library is loaded
+_type_codes = {}  # a2a_type of a torch type
 
 
 def _refuse(where: str, why: str):
     raise A2AError(ERR_INVALID_ARG, f"{where}: {why}")
 
 
-def _whole(where: str, name: str, t, dtype: str, shape) -> int:
+def _whole(where: str, name: str, t, dtype, shape) -> int:
     """Address of a contiguous device tensor of that type and shape."""
-    if str(t.dtype) != dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
         _refuse(where, f"{name} has to be a contiguous {dtype} device tensor of shape {tuple(shape)}")
     return t.data_ptr()
 
 
 def _rows(where: str, name: str, t, codes):
     """Type and distance of the rows of a device matrix whose numbers lie next to each other in a row."""
-    code = _type_code(t.dtype)
-    if code not in codes or t.dim() != 2 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1 and t.numel() > 0):
-        _refuse(where, f"{name} has to be a device matrix of one of the types in the header, its rows' numbers next to each other")
-    return code, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    code = _type_codes.get(t.dtype)
+    if code not in codes or not t.is_cuda or t.dim() != 2:
+        _refuse(where, f"{name} has to be a device matrix of one of the types in the header")
+    stride, step = t.stride()
+    if step != 1 and t.shape[1] > 1 and t.numel() > 0:
+        _refuse(where, f"{name} has to have the numbers of a row next to each other")
+    return code, stride if t.shape[0] > 1 else t.shape[1]
 
 
 def _routing(where: str, src_count: int, host_begin, experts: int, expert_host, *, choices=None, tokens=0, choices_per_token=0):
-    r = Routing(tokens, choices_per_token, experts)
+    kind = at = stride = 0
     if choices is not None:
-        r.choices_type, r.choices_stride = _rows(where, "choices", choices, (3, 4))
-        r.tokens, r.choices_per_token = choices.shape
-        r.choices = choices.data_ptr()
-    r.host_begin = _whole(where, "host_begin", host_begin, "torch.int64", (src_count + 1,))
-    if expert_host is not None:
-        r.expert_host = _whole(where, "expert_host", expert_host, "torch.int32", (experts,))
-    return r
+        kind, stride = _rows(where, "choices", choices, (3, 4))
+        tokens, choices_per_token = choices.shape
+        at = choices.data_ptr()
+    return Routing(tokens, choices_per_token, experts, kind, 0, at, stride,
+                   _whole(where, "host_begin", host_begin, _torch.int64, (src_count + 1,)),
+                   None if expert_host is None else _whole(where, "expert_host", expert_host, _torch.int32, (experts,)))
 
 
 def _stream(stream) -> Optional[int]:
-    import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream or None
+    if stream is None:  # (an object for it is most of a microsecond)
+        return _torch._C._cuda_getCurrentRawStream(_torch._C._cuda_getDevice()) or None
+    return stream.cuda_stream or None
 
 
 class Topology:
@@ -371,10 +367,10 @@ class Topology:
         the demands of :meth:`link_loads_demand` (there by target, here by source)."""
         where, shape = "a2a_path_costs", (src_count, self.N)
         return _check(load_library().a2a_path_costs(
-            self._h, src_begin, src_count, _whole(where, "dist", dist, "torch.int32", shape),
-            _whole(where, "sigma", sigma, "torch.float64", shape),
-            None if link_cost is None else _whole(where, "link_cost", link_cost, "torch.float64", (self.E,)),
-            _whole(where, "cost", cost, "torch.float64", shape), _ptr(workspace),
+            self._h, src_begin, src_count, _whole(where, "dist", dist, _torch.int32, shape),
+            _whole(where, "sigma", sigma, _torch.float64, shape),
+            None if link_cost is None else _whole(where, "link_cost", link_cost, _torch.float64, (self.E,)),
+            _whole(where, "cost", cost, _torch.float64, shape), _ptr(workspace),
             workspace.numel() if workspace is not None else 0, _stream(stream)), where)
 
     def dispatch_counts(self, src_count: int, *, choices, host_begin, experts: int, counts, stream=None) -> int:
@@ -384,7 +380,7 @@ class Topology:
         where = "a2a_dispatch_counts"
         r = _routing(where, src_count, host_begin, experts, None, choices=choices)
         return _check(load_library().a2a_dispatch_counts(
-            self._h, src_count, r, _whole(where, "counts", counts, "torch.int32", (src_count, experts)), _stream(stream)), where)
+            self._h, src_count, r, _whole(where, "counts", counts, _torch.int32, (src_count, experts)), _stream(stream)), where)
 
     def dispatch_demand(self, src_count: int, *, choices, host_begin, experts: int, expert_host=None, once: bool = False,
                         demand, stream=None) -> int:
@@ -394,7 +390,7 @@ class Topology:
         where = "a2a_dispatch_demand"
         r = _routing(where, src_count, host_begin, experts, expert_host, choices=choices)
         return _check(load_library().a2a_dispatch_demand(
-            self._h, src_count, r, int(once), _whole(where, "demand", demand, "torch.float64", (self.N, src_count)),
+            self._h, src_count, r, int(once), _whole(where, "demand", demand, _torch.float64, (self.N, src_count)),
             _stream(stream)), where)
 
     def balance_workspace_bytes(self, src_count: int, *, tokens: int, experts: int) -> int:
@@ -420,10 +416,10 @@ class Topology:
         shape = (src_count, experts)
         return _check(load_library().a2a_balance_loss(
             self._h, src_count, r, logits.data_ptr(), kind, stride,
-            None if cost is None else _whole(where, "cost", cost, "torch.float64", (src_count, self.N)),
-            _whole(where, "loss", loss, "torch.float32", (1,)), _whole(where, "counts", counts, "torch.int32", shape),
-            _whole(where, "prob_sums", prob_sums, "torch.float32", shape),
-            _whole(where, "rows", rows, "torch.int32", (src_count,)), _ptr(workspace),
+            None if cost is None else _whole(where, "cost", cost, _torch.float64, (src_count, self.N)),
+            _whole(where, "loss", loss, _torch.float32, (1,)), _whole(where, "counts", counts, _torch.int32, shape),
+            _whole(where, "prob_sums", prob_sums, _torch.float32, shape),
+            _whole(where, "rows", rows, _torch.int32, (src_count,)), _ptr(workspace),
             workspace.numel() if workspace is not None else 0, _stream(stream)), where)
 
     def balance_loss_grad(self, src_count: int, *, logits, choices_per_token: int, host_begin, cost=None, expert_host=None,
@@ -439,10 +435,10 @@ class Topology:
         r = _routing(where, src_count, host_begin, experts, expert_host, tokens=tokens, choices_per_token=choices_per_token)
         return _check(load_library().a2a_balance_loss_grad(
             self._h, src_count, r, logits.data_ptr(), kind, stride,
-            None if cost is None else _whole(where, "cost", cost, "torch.float64", (src_count, self.N)),
-            _whole(where, "counts", counts, "torch.int32", (src_count, experts)),
-            _whole(where, "rows", rows, "torch.int32", (src_count,)),
-            None if upstream is None else _whole(where, "upstream", upstream, "torch.float32", (1,)),
+            None if cost is None else _whole(where, "cost", cost, _torch.float64, (src_count, self.N)),
+            _whole(where, "counts", counts, _torch.int32, (src_count, experts)),
+            _whole(where, "rows", rows, _torch.int32, (src_count,)),
+            None if upstream is None else _whole(where, "upstream", upstream, _torch.float32, (1,)),
             grad.data_ptr(), grad_stride, _stream(stream)), where)
 
     def profile_enable(self, mode: int = 1) -> None:

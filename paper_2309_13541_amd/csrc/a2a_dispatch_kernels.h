@@ -38,42 +38,190 @@ __device__ __forceinline__ int begun(const int64_t* __restrict__ begin, int entr
 // counts and demands
 // ---------------------------------------------------------------------------------------
 
-template <typename Id>
-__device__ __forceinline__ int host_of(const Routing& r, long long t, int j, int hosts) {
-  const Id e = ((const Id*)r.choices)[t * r.stride + j];
-  if (e < 0 || e >= r.experts) return -1;
-  const int h = r.expert_host ? r.expert_host[e] : (int)e;
-  return h >= 0 && h < hosts ? h : -1;
+// Cells are counted in LDS, by a workgroup that has them to itself (k_dispatch_tiles) or has some tokens of a source
+// (k_dispatch_split).  Whole numbers: no order of additions matters.  What a choice counts for is a row: the expert
+// (counts) or its host (demands).
+struct Dispatch {
+  Routing r;
+  int rows, once;   // rows: experts or hosts
+  int tile, tiles;  // rows of a workgroup
+  int columns;      // sources of a workgroup
+  long long per;    // tokens of a workgroup (k_dispatch_split)
+  int32_t* counts;  // [sources][rows]
+  double* demand;   // [rows][sources]
+};
+
+// Row of choice number i of the tokens from t0 on, and its token; -1: none.
+template <typename Id, bool kDemand>
+struct Choices {
+  const Routing& r;
+  const Id* at;
+  int rows;
+  bool once, dense;
+  unsigned k;
+  __device__ __forceinline__ Choices(const Dispatch& d, long long t0)
+      : r(d.r), at((const Id*)d.r.choices + t0 * d.r.stride), rows(d.rows), once(d.once != 0), dense(d.r.stride == d.r.k), k(d.r.k) {}
+  __device__ __forceinline__ Id raw(unsigned i) const { return dense ? at[i] : at[(long long)(i / k) * r.stride + i % k]; }
+  __device__ __forceinline__ int row_of(Id e) const {
+    if (e < 0 || e >= r.experts) return -1;
+    if constexpr (!kDemand) return (int)e;
+    const int h = r.expert_host ? r.expert_host[e] : (int)e;
+    return (unsigned)h < (unsigned)rows ? h : -1;
+  }
+};
+
+// f(i, row) for the choices i of n that a thread has and that count: of all, four of them asked for at a time; or of every
+// token the first for each host, eight choices of a token at a time.
+template <typename Id, bool kDemand, typename F>
+__device__ __forceinline__ void each_row(const Choices<Id, kDemand>& c, unsigned n, F&& f) {
+  if (kDemand && c.once) {
+    constexpr unsigned kAhead = 8;
+    const auto hosts = [&](unsigned i, unsigned left, int (&h)[kAhead]) {
+      Id e[kAhead];
+#pragma unroll
+      for (unsigned q = 0; q < kAhead; ++q) e[q] = q < left ? c.raw(i + q) : (Id)-1;
+#pragma unroll
+      for (unsigned q = 0; q < kAhead; ++q) h[q] = c.row_of(e[q]);
+    };
+    for (unsigned t = threadIdx.x; t < n / c.k; t += blockDim.x)
+      for (unsigned j = 0; j < c.k; j += kAhead) {
+        int h[kAhead], before[kAhead];
+        hosts(t * c.k + j, c.k - j, h);
+#pragma unroll
+        for (unsigned q = 1; q < kAhead; ++q)
+#pragma unroll
+          for (unsigned p = 0; p < q; ++p) h[q] = h[q] == h[p] ? -1 : h[q];
+        for (unsigned i = 0; i < j; i += kAhead) {
+          hosts(t * c.k + i, kAhead, before);
+#pragma unroll
+          for (unsigned q = 0; q < kAhead; ++q)
+#pragma unroll
+            for (unsigned p = 0; p < kAhead; ++p) h[q] = h[q] == before[p] ? -1 : h[q];
+        }
+#pragma unroll
+        for (unsigned q = 0; q < kAhead; ++q)
+          if (h[q] >= 0) f(t * c.k + j + q, h[q]);
+      }
+    return;
+  }
+  constexpr unsigned kAhead = 4;
+  for (unsigned i0 = threadIdx.x; i0 < n; i0 += kAhead * blockDim.x) {
+    Id e[kAhead];
+#pragma unroll
+    for (unsigned q = 0; q < kAhead; ++q) {
+      const unsigned i = i0 + q * blockDim.x;
+      e[q] = i < n ? c.raw(i) : (Id)-1;
+    }
+#pragma unroll
+    for (unsigned q = 0; q < kAhead; ++q) {
+      const int h = c.row_of(e[q]);
+      if (h >= 0) f(i0 + q * blockDim.x, h);
+    }
+  }
 }
 
 static __global__ void __launch_bounds__(kBlock) k_fill(int32_t* p, size_t n) {
   for (size_t i = (size_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += (size_t)gridDim.x * kBlock) p[i] = 0;
 }
 
-// A thread per choice, and an atomic addition for each.  Whole numbers below 2^53: the order does not matter.
+// host_begin as it may be used: within the tokens
+__device__ __forceinline__ long long begin_of(const Routing& r, int s) {
+  return min(max((long long)r.host_begin[s], 0ll), r.tokens);
+}
+
+// A band of `columns` sources and `tile` rows a workgroup, which reads these sources' tokens and writes the cells.  A cell has 16
+// bits where the band has less than 65536 choices; where it has more, 32, and the rows go in two halves, each with a pass over
+// the tokens.
 template <typename Id, bool kDemand>
-__global__ void __launch_bounds__(kBlock) k_dispatch(Routing r, int hosts, int once, int32_t* counts, double* demand) {
-  const long long i = (long long)blockIdx.x * kBlock + threadIdx.x;
-  if (i >= r.tokens * r.k) return;
-  const long long t = i / r.k;
-  const int j = (int)(i - t * r.k);
-  int lo = 0, hi = r.sources + 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (r.host_begin[mid] <= t) lo = mid + 1; else hi = mid;
+__global__ void __launch_bounds__(kDispatchThreads) k_dispatch_tiles(Dispatch d) {
+  extern __shared__ uint32_t cells[];  // demands: [rows][columns]
+  __shared__ long long begin[kDispatchColumns + 1];
+  __shared__ unsigned behind[kDispatchColumns];  // of the first choice of the band, behind the last one of a source
+  const int T = blockDim.x;
+  const int s0 = blockIdx.x / d.tiles * d.columns;
+  const int columns = min(d.columns, d.r.sources - s0), band_rows = min(d.tile, d.rows - blockIdx.x % d.tiles * d.tile);
+  if ((int)threadIdx.x <= columns) begin[threadIdx.x] = begin_of(d.r, s0 + threadIdx.x);
+  __syncthreads();
+  const long long t0 = begin[0];
+  const unsigned k = d.r.k, n = begin[columns] > t0 ? (unsigned)(begin[columns] - t0) * k : 0;
+  if ((int)threadIdx.x < kDispatchColumns)
+    behind[threadIdx.x] = (int)threadIdx.x < columns ? (unsigned)(max(begin[threadIdx.x + 1], t0) - t0) * k : ~0u;
+  const Choices<Id, kDemand> c(d, t0);
+  const bool narrow = n < 65536u;
+  const int part = narrow ? d.tile : (d.tile + 1) / 2;
+  for (int done = 0; done < band_rows; done += part) {
+    const int row0 = blockIdx.x % d.tiles * d.tile + done, rows = min(part, band_rows - done), size = rows * columns;
+    const int words = narrow ? (size + 1) / 2 : size;
+    for (int i = threadIdx.x; i < words; i += T) cells[i] = 0;
+    __syncthreads();
+    each_row<Id, kDemand>(c, n, [&](unsigned i, int h) {
+      const unsigned row = (unsigned)(h - row0);
+      if (row >= (unsigned)rows) return;
+      unsigned s = 0;
+      if constexpr (kDemand) {
+#pragma unroll
+        for (int half = kDispatchColumns / 2; half > 0; half /= 2) s += behind[s + half - 1] <= i ? half : 0;
+      }
+      const unsigned at = row * columns + s;
+      narrow ? atomicAdd(&cells[at / 2], at & 1u ? 0x10000u : 1u) : atomicAdd(&cells[at], 1u);
+    });
+    __syncthreads();
+    const auto cell = [&](int i) { return narrow ? cells[i / 2] >> (i & 1 ? 16 : 0) & 0xffffu : cells[i]; };
+    if constexpr (kDemand) {
+      if (columns == kDispatchColumns) {
+        for (int i = threadIdx.x; i < size; i += T)
+          d.demand[(size_t)(row0 + i / kDispatchColumns) * d.r.sources + s0 + i % kDispatchColumns] = (double)cell(i);
+      } else {
+        for (int i = threadIdx.x; i < size; i += T)
+          d.demand[(size_t)(row0 + i / columns) * d.r.sources + s0 + i % columns] = (double)cell(i);
+      }
+    } else {
+      for (int i = threadIdx.x; i < rows; i += T) d.counts[(size_t)s0 * d.rows + row0 + i] = (int32_t)cell(i);
+    }
+    __syncthreads();
   }
-  const int s = lo - 1;
-  if (s < 0 || s >= r.sources) return;
-  if constexpr (kDemand) {
-    const int h = host_of<Id>(r, t, j, hosts);
-    if (h < 0) return;
-    if (once)
-      for (int i = 0; i < j; ++i)
-        if (host_of<Id>(r, t, i, hosts) == h) return;
-    unsafeAtomicAdd(demand + (size_t)h * r.sources + s, 1.0);
-  } else {
-    const Id e = ((const Id*)r.choices)[t * r.stride + j];
-    if (e >= 0 && e < r.experts) atomicAdd(counts + (size_t)s * r.experts + e, 1);
+}
+
+// `per` tokens a workgroup, their sources one after the other, into cells that are 0 before.
+template <typename Id, bool kDemand>
+__global__ void __launch_bounds__(kDispatchThreads) k_dispatch_split(Dispatch d) {
+  extern __shared__ uint32_t cells[];  // [tile]
+  const int T = blockDim.x;
+  const int row0 = blockIdx.x % d.tiles * d.tile, rows = min(d.tile, d.rows - row0);
+  long long t = (long long)(blockIdx.x / d.tiles) * d.per;
+  const long long end = min(t + d.per, d.r.tokens);
+  const auto add = [&](int s, int row, unsigned n) {
+    if constexpr (kDemand)
+      unsafeAtomicAdd(d.demand + (size_t)(row0 + row) * d.r.sources + s, (double)n);
+    else
+      atomicAdd(d.counts + (size_t)s * d.rows + row0 + row, (int)n);
+  };
+  while (t < end) {
+    const int n = begun(d.r.host_begin, d.r.sources + 1, t);
+    if (n > d.r.sources) break;
+    const long long next = max(min(end, (long long)d.r.host_begin[n]), t + 1);
+    if (n > 0) {
+      const unsigned choices = (unsigned)(next - t) * d.r.k;
+      const Choices<Id, kDemand> c(d, t);
+      if (choices < (unsigned)rows / 4) {  // fewer than there are cells to look through
+        each_row<Id, kDemand>(c, choices, [&](unsigned, int h) {
+          const unsigned row = (unsigned)(h - row0);
+          if (row < (unsigned)rows) add(n - 1, (int)row, 1);
+        });
+      } else {
+        for (int i = threadIdx.x; i < rows; i += T) cells[i] = 0;
+        __syncthreads();
+        each_row<Id, kDemand>(c, choices, [&](unsigned, int h) {
+          const unsigned row = (unsigned)(h - row0);
+          if (row < (unsigned)rows) atomicAdd(&cells[row], 1u);
+        });
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows; i += T)
+          if (cells[i] != 0) add(n - 1, i, cells[i]);
+        __syncthreads();
+      }
+    }
+    t = next;
   }
 }
 

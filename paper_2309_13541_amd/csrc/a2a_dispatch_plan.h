@@ -51,6 +51,44 @@ inline int check_logits(const a2a_routing* r, const void* logits, int type, int6
   return A2A_OK;
 }
 
+// Counts and demands.  A workgroup has a band of sources to itself, reads their tokens and writes their cells once; sources with
+// many tokens are split over workgroups that add to cells set to 0 before.
+constexpr int kDispatchThreads = 1024;
+constexpr int kDispatchColumns = 16;    // sources of a band at the most: 128 bytes of a row of demands
+constexpr int kDispatchCells = 65536;   // cells of 16 bits: 128 KB of LDS
+struct DispatchCut {
+  bool split = false;
+  int columns = 1, tile = 1, tiles = 1, threads = 256;
+  int64_t per = 0, groups = 0;  // tokens of a workgroup that splits; workgroups
+  size_t lds = 0;
+};
+inline DispatchCut dispatch_cut(int64_t sources, int64_t tokens, int64_t choices_per_token, int64_t rows, bool demand) {
+  DispatchCut c;
+  const int64_t choices = tokens * choices_per_token;
+  // as many sources a band as leave 256 bands
+  while (demand && c.columns < kDispatchColumns && sources >= 512 * c.columns) c.columns *= 2;
+  const int64_t bands = (sources + c.columns - 1) / c.columns;
+  // pieces of the split form, with a pass over the rows' cells each
+  const int64_t per = std::max<int64_t>((tokens + 1023) / 1024, (1024 + choices_per_token - 1) / choices_per_token);
+  const int64_t pieces = (tokens + per - 1) / per + sources;
+  c.split = bands < 256 ? choices / bands > 16384 : !demand && choices / pieces > 4 * rows;
+  if (c.split) {
+    c.columns = 1;
+    c.tile = (int)std::min<int64_t>(rows, kDispatchCells / 4);
+    c.tiles = (int)((rows + c.tile - 1) / c.tile);
+    c.per = per;
+    c.groups = (tokens + per - 1) / per * c.tiles;
+    c.lds = (size_t)c.tile * 4;
+  } else {
+    c.tile = (int)std::min<int64_t>(rows, kDispatchCells / c.columns);
+    c.tiles = (int)((rows + c.tile - 1) / c.tile);
+    c.groups = bands * c.tiles;
+    c.lds = ((size_t)(c.tile + 1) / 2 * c.columns + 1) * 4;  // of 16 bits each, or of 32 for half of the rows
+    if (demand && choices / bands > 1024) c.threads = kDispatchThreads;
+  }
+  return c;
+}
+
 // Passes over logits: a workgroup has `per` consecutive tokens, of as many sources as they belong to.  The tokens of
 // workgroup b that belong to source s are its piece (b, s).  Pieces follow each other, and from one to the next b or s
 // grows, so b + s numbers them: the sums of a piece have place b + s of the workspace, and those of source s are the

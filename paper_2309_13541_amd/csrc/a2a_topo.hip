@@ -1238,21 +1238,37 @@ int dispatch(const a2a_topo* t, int32_t src_count, const a2a_routing* routing, i
   const Use use(t, st);
   const Routing r = routing_of(routing, src_count);
   ProfScope ps(t, PROF_TOKENS, st);
-  if (counts) {
-    const size_t cells = (size_t)src_count * r.experts;
-    k_fill<<<(unsigned)std::min<size_t>((cells + kBlock - 1) / kBlock, 16384), kBlock, 0, st>>>(counts, cells);
-  } else {
-    HIP_TRY(zero_async(demand, (size_t)t->N * src_count * 8, st));
+  Dispatch d{};
+  d.r = r;
+  d.rows = counts ? r.experts : t->N;
+  d.once = once;
+  d.counts = counts;
+  d.demand = demand;
+  const DispatchCut cut = dispatch_cut(src_count, r.tokens, r.k, d.rows, counts == nullptr);
+  d.tile = cut.tile;
+  d.tiles = cut.tiles;
+  d.columns = cut.columns;
+  d.per = cut.per;
+  if (cut.split) {
+    if (counts) {
+      const size_t cells = (size_t)src_count * d.rows;
+      k_fill<<<(unsigned)std::min<size_t>((cells + kBlock - 1) / kBlock, 16384), kBlock, 0, st>>>(counts, cells);
+    } else {
+      HIP_TRY(zero_async(demand, (size_t)d.rows * src_count * 8, st));
+    }
   }
-  const unsigned blocks = (unsigned)((r.tokens * r.k + kBlock - 1) / kBlock);
-  if (blocks > 0) {
-    const bool wide = routing->choices_type == A2A_I64;
-    const auto launch = [&](auto kernel) { kernel<<<blocks, kBlock, 0, st>>>(r, t->N, once, counts, demand); };
-    if (counts)
-      wide ? launch(k_dispatch<int64_t, false>) : launch(k_dispatch<int32_t, false>);
-    else
-      wide ? launch(k_dispatch<int64_t, true>) : launch(k_dispatch<int32_t, true>);
-  }
+  const auto launch = [&](auto kernel) {
+    kernel<<<(unsigned)cut.groups, cut.threads, cut.lds, st>>>(d);
+  };
+  const bool wide = routing->choices_type == A2A_I64;
+  if (cut.split && counts)
+    wide ? launch(k_dispatch_split<int64_t, false>) : launch(k_dispatch_split<int32_t, false>);
+  else if (cut.split)
+    wide ? launch(k_dispatch_split<int64_t, true>) : launch(k_dispatch_split<int32_t, true>);
+  else if (counts)
+    wide ? launch(k_dispatch_tiles<int64_t, false>) : launch(k_dispatch_tiles<int32_t, false>);
+  else
+    wide ? launch(k_dispatch_tiles<int64_t, true>) : launch(k_dispatch_tiles<int32_t, true>);
   HIP_TRY(hipGetLastError());
   return A2A_OK;
 }
