@@ -244,7 +244,8 @@ struct Balance {
   int32_t* counts;
   int32_t* rows;
   // the call's
-  double* terms;
+  double* terms;      // [workgroups of k_balance_sources][2]
+  int across, wide_choices;
   float* out_loss;
   int32_t* out_counts;
   float* out_sums;
@@ -259,8 +260,7 @@ struct Balance {
 
 template <int kCtrl>
 __device__ __forceinline__ float dpp(float x) {
-  const int i = __float_as_int(x);
-  return __int_as_float(__builtin_amdgcn_update_dpp(i, i, kCtrl, 0xf, 0xf, false));
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kCtrl, 0xf, 0xf, true));
 }
 
 // f over the kLanes lanes of a row, in all of them.  Lanes of a quad, then of halves and wholes of 16 (mirrored: the quads
@@ -280,8 +280,10 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__bf16 x) { return (float)x; }
 __device__ __forceinline__ float to_float(_Float16 x) { return (float)x; }
 
-// The numbers of a row that a lane has.  Pieces of 16 bytes (kWide: rows begin at multiples of 16 bytes) or one number at
-// a time, neighbours in neighbouring lanes.
+// The numbers of a row that a lane has: pieces of 16 bytes (kWide: rows begin at multiples of 16 bytes and end at one), or one
+// number at a time, neighbours in neighbouring lanes.  Requests for a row have no conditions, so that the next one's can be
+// counted while this one's are waited for: a lane with a place past the row's end asks for the row's first piece and has
+// -infinity in its place.
 template <typename T, bool kWide, int kLanes, int kValues>
 struct Row {
   static constexpr int kPiece = kWide ? 16 / (int)sizeof(T) : 1;
@@ -292,29 +294,22 @@ struct Row {
   static __device__ __forceinline__ int expert(int lane, int i) {  // of a lane's number i
     return (i / kPiece * kLanes + lane) * kPiece + i % kPiece;
   }
-  __device__ __forceinline__ void load(const T* __restrict__ row, int lane, int experts) {
+  __device__ __forceinline__ void load(const T* row, int lane, int experts) {
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
       const int e = expert(lane, q * kPiece);
-      if (e + kPiece <= experts) {
-        p[q] = *reinterpret_cast<const Piece*>(row + e);
-      } else {
-#pragma unroll
-        for (int j = 0; j < kPiece; ++j) p[q][j] = e + j < experts ? row[e + j] : (T)-INFINITY;
-      }
+      p[q] = *reinterpret_cast<const Piece*>(row + (e < experts ? e : 0));
     }
+  }
+  __device__ __forceinline__ void cut(int lane, int experts) {
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) p[q] = expert(lane, q * kPiece) < experts ? p[q] : (Piece)(T)-INFINITY;
   }
   __device__ __forceinline__ void store(T* __restrict__ row, int lane, int experts) const {
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
       const int e = expert(lane, q * kPiece);
-      if (e + kPiece <= experts) {
-        *reinterpret_cast<Piece*>(row + e) = p[q];
-      } else {
-#pragma unroll
-        for (int j = 0; j < kPiece; ++j)
-          if (e + j < experts) row[e + j] = p[q][j];
-      }
+      if (e < experts) *reinterpret_cast<Piece*>(row + e) = p[q];
     }
   }
   __device__ __forceinline__ float get(int i) const { return to_float(p[i / kPiece][i % kPiece]); }
@@ -327,7 +322,7 @@ struct Row {
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kValues; ++i) top = fmaxf(top, get(i));
-    top = over_lanes<kLanes>(top, [](float a, float b) { return fmaxf(a, b); });
+    top = over_lanes<kLanes>(top, [](float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); });  // the larger one
     constexpr float kLog2e = 1.44269504088896340736f;
     top = top == -INFINITY ? 0.0f : top;
     float sum = 0.0f;
@@ -340,73 +335,124 @@ struct Row {
   }
 };
 
-// The pieces of workgroup b, in order: f(source, first token, token behind the last).
+// The pieces of workgroup b, in order: f(source, first token, token behind the last).  The end of the source after comes with
+// the end of each, so that only sources behind empty ones are looked for.
 template <typename F>
 __device__ __forceinline__ void for_pieces(const Routing& r, long long per, F&& f) {
   long long t = (long long)blockIdx.x * per;
   const long long end = min(t + per, r.tokens);
-  while (t < end) {
-    const int n = begun(r.host_begin, r.sources + 1, t);
-    if (n > r.sources) break;                            // behind the last source's tokens
-    long long next = min(end, (long long)r.host_begin[n]);
-    next = max(next, t + 1);
+  if (t >= end) return;
+  int n = begun(r.host_begin, r.sources + 1, t);  // entries that are at most t
+  while (n <= r.sources) {                        // not behind the last source's tokens
+    const long long stop = r.host_begin[n], after = r.host_begin[min(n + 1, r.sources)];
+    const long long next = max(min(end, stop), t + 1);
     if (n > 0) f(n - 1, t, next);
     t = next;
+    if (t >= end) break;
+    n = stop == t && after > t ? n + 1 : begun(r.host_begin, r.sources + 1, t);
   }
 }
 
-template <typename T, bool kWide, int kLanes, int kValues, typename Id>
+// Sum over the rows that a wave has at a time, in the first row's lanes.
+template <int kLanes>
+__device__ __forceinline__ float over_rows(float x) {
+  if constexpr (kLanes <= 1) x += dpp<0x121>(x);  // rotations within 16 lanes
+  if constexpr (kLanes <= 2) x += dpp<0x122>(x);
+  if constexpr (kLanes <= 4) x += dpp<0x124>(x);
+  if constexpr (kLanes <= 8) x += dpp<0x128>(x);
+  if constexpr (kLanes <= 16) x += __shfl_xor(x, 16, kWave);
+  if constexpr (kLanes <= 32) x += __shfl_xor(x, 32, kWave);
+  return x;
+}
+
+// Whether a lane asks for its next row before it works on the one it has: not where their registers are too many.
+constexpr bool row_ahead(int values) { return values <= 40; }
+
+template <typename T, bool kWide, int kLanes, int kValues>
 __global__ void __launch_bounds__(kBalanceThreads) k_balance_rows(Balance b) {
   using R = Row<T, kWide, kLanes, kValues>;
-  constexpr int kWaves = kBalanceThreads / kWave, kRows = kWave / kLanes;
+  constexpr int kWaves = kBalanceThreads / kWave, kRows = kWave / kLanes, kStep = kWaves * kRows;
   extern __shared__ float lds[];  // [kWaves][experts] sums, int [experts] counts, int [kWaves] rows
   const int X = b.r.experts, k = b.r.k;
   int* const counts = (int*)(lds + kWaves * X);
   int* const rows = counts + X;
   const int wave = threadIdx.x / kWave, lane = lane_id() % kLanes, slot = lane_id() / kLanes;
+  // the words of a choice as they come, and the expert that they say
+  const int words = b.wide_choices ? 2 : 1;
+  const auto choice = [&](const int32_t* p) { return make_int2(p[0], p[words - 1]); };
+  const auto expert_of = [&](int2 e) { return (words == 1 || e.y == 0) && (unsigned)e.x < (unsigned)X ? e.x : -1; };
+  const long long row_step = b.logits_stride * kStep, choice_step = b.r.stride * words * kStep;
   for_pieces(b.r, b.per, [&](int s, long long t0, long long t1) {
-    for (int e = threadIdx.x; e < X; e += kBalanceThreads) counts[e] = 0;
+    R rows_of[2];  // a row is asked for while the one before is worked on; after the last one that again
+    int2 marks[2];
+    const int first = wave * kRows + slot, n = (int)(t1 - t0);
+    int left = n - first;
+    const T* at = (const T*)b.logits + (t0 + min(first, n - 1)) * b.logits_stride;
+    const int32_t* choices = (const int32_t*)b.r.choices + (t0 + min(first, n - 1)) * b.r.stride * words;
+    const auto fetch = [&](int i) {
+      rows_of[i].load(at, lane, X);
+      marks[i] = choice(choices + min(lane, k - 1) * words);
+    };
+    const auto next = [&] {
+      at += left > kStep ? row_step : 0;
+      choices += left > kStep ? choice_step : 0;
+    };
+    fetch(0);
+    for (int i = threadIdx.x; i < X; i += kBalanceThreads) counts[i] = 0;
     __syncthreads();
     float acc[kValues] = {};
     int mine = 0;
-    for (long long t = t0 + wave * kRows + slot; t - slot < t1; t += kWaves * kRows) {
-      float x[kValues], inv = 0.0f;
-      bool token = false;
-      if (t < t1) {
-        R row;
-        row.load((const T*)b.logits + t * b.logits_stride, lane, X);
-        const float sum = row.exponentials(x);
-        token = sum != 0.0f;
-        inv = token ? 1.0f / sum : 0.0f;
+    const auto work = [&](int i, const int32_t* of_row) {
+      float x[kValues];
+      rows_of[i].cut(lane, X);
+      const float sum = rows_of[i].exponentials(x);
+      const float inv = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);
 #pragma unroll
-        for (int i = 0; i < kValues; ++i) acc[i] = __builtin_fmaf(x[i], inv, acc[i]);
-        if (token) {
-          mine += lane == 0;
-          for (int j = lane; j < k; j += kLanes) {
-            const Id e = ((const Id*)b.r.choices)[t * b.r.stride + j];
-            if (e >= 0 && e < X) atomicAdd(&counts[e], 1);
-          }
-        }
+      for (int j = 0; j < kValues; ++j) acc[j] = __builtin_fmaf(x[j], inv, acc[j]);
+      if (sum == 0.0f) return;
+      mine += lane == 0;
+      const int e = lane < k ? expert_of(marks[i]) : -1;
+      if (e >= 0) atomicAdd(&counts[e], 1);
+      for (int j = lane + kLanes; j < k; j += kLanes) {
+        const int more = expert_of(choice(of_row + j * words));
+        if (more >= 0) atomicAdd(&counts[more], 1);
       }
+    };
+    while (left > 0) {
+      const int32_t* const of_row = choices;
+      next();
+      if constexpr (row_ahead(kValues)) {
+        fetch(1);
+        work(0, of_row);
+        left -= kStep;
+        if (left <= 0) break;
+        const int32_t* const of_next = choices;
+        next();
+        fetch(0);
+        work(1, of_next);
+      } else {
+        work(0, of_row);
+        fetch(0);
+      }
+      left -= kStep;
     }
 #pragma unroll
     for (int i = 0; i < kValues; ++i) {
-#pragma unroll
-      for (int m = kLanes; m < kWave; m *= 2) acc[i] += __shfl_xor(acc[i], m, kWave);
-      const int e = R::expert(lane, i);
-      if (slot == 0 && e < X) lds[wave * X + e] = acc[i];
+      const float sum = over_rows<kLanes>(acc[i]);
+      const int at = R::expert(lane, i);
+      if (slot == 0 && at < X) lds[wave * X + at] = sum;
     }
 #pragma unroll
-    for (int m = kLanes; m < kWave; m *= 2) mine += __shfl_xor(mine, m, kWave);
+    for (int m = 1; m < kWave; m *= 2) mine += __shfl_xor(mine, m, kWave);
     if (lane_id() == 0) rows[wave] = mine;
     __syncthreads();
     const size_t place = (size_t)blockIdx.x + s;
-    for (int e = threadIdx.x; e < X; e += kBalanceThreads) {
-      float sum = lds[e];
+    for (int i = threadIdx.x; i < X; i += kBalanceThreads) {
+      float sum = lds[i];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) sum += lds[w * X + e];
-      b.sums[place * X + e] = sum;
-      b.counts[place * X + e] = counts[e];
+      for (int w = 1; w < kWaves; ++w) sum += lds[w * X + i];
+      b.sums[place * X + i] = sum;
+      b.counts[place * X + i] = counts[i];
     }
     if (threadIdx.x == 0) {
       int n = 0;
@@ -437,51 +483,90 @@ __device__ __forceinline__ double block_sum(double x, double* lds) {
   return sum;
 }
 
-// A source's pieces, added up in the order of its tokens, and its term of the loss: double precision from here on.
+// A source's pieces added up, `across` of them at a time beside each other, for kBalanceThreads / across experts; where one
+// at a time is enough (across 1) the cells of several sources beside each other: an item.  Double precision from here on.  A
+// workgroup has every gridDim.x-th item and leaves the sum of their terms.  All in an order that the sizes alone decide.
 static __global__ void __launch_bounds__(kBalanceThreads) k_balance_sources(Balance b) {
-  __shared__ double lds[kBalanceThreads / kWave];
-  const int s = blockIdx.x, X = b.r.experts;
-  const long long first = min(max((long long)b.r.host_begin[s], 0ll), b.r.tokens);
-  const long long behind = min((long long)b.r.host_begin[s + 1], b.r.tokens);
-  const long long b0 = first / b.per, b1 = behind > first ? (behind - 1) / b.per : b0 - 1;
-  int rows = 0;
-  for (long long g = b0; g <= b1; ++g) rows += b.rows[g + s];
-  double term = 0.0;
-  for (int e = threadIdx.x; e < X; e += kBalanceThreads) {
-    double sum = 0.0;
-    int count = 0;
-    for (long long g = b0; g <= b1; ++g) {
-      sum += b.sums[(g + s) * X + e];
-      count += b.counts[(g + s) * X + e];
+  __shared__ double lds[kBalanceThreads], waves[kBalanceThreads / kWave];
+  __shared__ int lds_counts[kBalanceThreads], lds_rows[kBalanceThreads];
+  const int X = b.r.experts, across = b.across, experts = kBalanceThreads / across, parts = (X + experts - 1) / experts;
+  const int i = threadIdx.x % experts, lane = threadIdx.x / experts;
+  const long long cells = (long long)b.r.sources * X;
+  const long long items = across > 1 ? (long long)b.r.sources * parts : (cells + kBalanceThreads - 1) / kBalanceThreads;
+  double terms = 0.0, all_rows = 0.0;
+  for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+    int s = (int)(item / parts), e = (int)(item % parts) * experts + i;
+    if (across == 1) {
+      const long long cell = min(item * kBalanceThreads + threadIdx.x, cells - 1);
+      s = (int)(cell / X);
+      e = item * kBalanceThreads + threadIdx.x < cells ? (int)(cell % X) : X;
     }
-    b.out_sums[(size_t)s * X + e] = (float)sum;
-    b.out_counts[(size_t)s * X + e] = count;
-    if (rows > 0) term += weight_of(b, s, e) * count * sum;
+    const long long first = begin_of(b.r, s), behind = begin_of(b.r, s + 1);
+    const long long g0 = first / b.per, g1 = behind > first ? (behind - 1) / b.per : g0 - 1;
+    double sum = 0.0;
+    int count = 0, rows = 0;
+#pragma unroll 8
+    for (long long g = g0 + lane; g <= g1; g += across) {
+      rows += b.rows[g + s];
+      if (e < X) {
+        sum += b.sums[(g + s) * X + e];
+        count += b.counts[(g + s) * X + e];
+      }
+    }
+    if (across > 1) {
+      lds[threadIdx.x] = sum;
+      lds_counts[threadIdx.x] = count;
+      lds_rows[threadIdx.x] = rows;
+      __syncthreads();
+      for (int half = across / 2; half > 0; half /= 2) {
+        if (lane < half) {
+          sum += lds[threadIdx.x + half * experts];
+          count += lds_counts[threadIdx.x + half * experts];
+          rows += lds_rows[threadIdx.x + half * experts];
+          lds[threadIdx.x] = sum;
+          lds_counts[threadIdx.x] = count;
+          lds_rows[threadIdx.x] = rows;
+        }
+        __syncthreads();
+      }
+    }
+    if (lane == 0 && e < X) {
+      b.out_sums[(size_t)s * X + e] = (float)sum;
+      b.out_counts[(size_t)s * X + e] = count;
+      if (rows > 0) terms += weight_of(b, s, e) * count * sum / rows;
+      if (e == 0) {
+        b.out_rows[s] = rows;
+        all_rows += rows;
+      }
+    }
   }
-  term = block_sum(term, lds);
+  terms = block_sum(terms, waves);
+  all_rows = block_sum(all_rows, waves);
   if (threadIdx.x == 0) {
-    b.out_rows[s] = rows;
-    b.terms[s] = rows > 0 ? term / rows : 0.0;
+    b.terms[2 * blockIdx.x] = terms;
+    b.terms[2 * blockIdx.x + 1] = all_rows;
   }
 }
 
-// The loss from the sources' terms.
-static __global__ void __launch_bounds__(kBalanceThreads) k_balance_loss(Balance b) {
-  __shared__ double lds[kBalanceThreads / kWave];
+// The loss from those sums.  (The last workgroup of k_balance_sources to come could add them up, but a release at the scope of
+// the device by every workgroup, with what it has written still in the caches, made that kernel 50 us for 1024 sources of 256
+// experts, where it takes 8 without.)
+static __global__ void __launch_bounds__(kBalanceThreads) k_balance_loss(Balance b, int groups) {
+  __shared__ double waves[kBalanceThreads / kWave];
   double sum = 0.0, rows = 0.0;
-  for (int s = threadIdx.x; s < b.r.sources; s += kBalanceThreads) {
-    sum += b.terms[s];
-    rows += b.out_rows[s];
+  for (int g = threadIdx.x; g < groups; g += kBalanceThreads) {
+    sum += b.terms[2 * g];
+    rows += b.terms[2 * g + 1];
   }
-  sum = block_sum(sum, lds);
-  rows = block_sum(rows, lds);
+  sum = block_sum(sum, waves);
+  rows = block_sum(rows, waves);
   if (threadIdx.x == 0) b.out_loss[0] = rows > 0.0 ? (float)(sum * b.r.experts / (b.r.k * rows)) : 0.0f;
 }
 
 template <typename T, bool kWide, int kLanes, int kValues>
 __global__ void __launch_bounds__(kBalanceThreads) k_balance_grad(Balance b) {
   using R = Row<T, kWide, kLanes, kValues>;
-  constexpr int kWaves = kBalanceThreads / kWave, kRows = kWave / kLanes;
+  constexpr int kWaves = kBalanceThreads / kWave, kRows = kWave / kLanes, kStep = kWaves * kRows;
   extern __shared__ double lds64[];  // [kWaves] doubles, float [experts]
   float* const coef = (float*)(lds64 + kWaves + 1);
   const int X = b.r.experts;
@@ -492,7 +577,15 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance_grad(Balance b) {
   if (threadIdx.x == 0) lds64[kWaves] = n > 0.0 ? (b.upstream ? (double)b.upstream[0] : 1.0) * X / (b.r.k * n) : 0.0;
   __syncthreads();
   const double scale = lds64[kWaves];
+  const long long row_step = b.logits_stride * kStep, grad_step = b.grad_stride * kStep;
   for_pieces(b.r, b.per, [&](int s, long long t0, long long t1) {
+    R rows_of[2];
+    const int first = wave * kRows + slot, n = (int)(t1 - t0);
+    int left = n - first;
+    const T* at = (const T*)b.logits + (t0 + min(first, n - 1)) * b.logits_stride;
+    T* to = (T*)b.grad + (t0 + min(first, n - 1)) * b.grad_stride;
+    const auto next = [&] { at += left > kStep ? row_step : 0; };
+    rows_of[0].load(at, lane, X);
     const double of_source = scale / max(b.in_rows[s], 1);
     for (int e = threadIdx.x; e < X; e += kBalanceThreads)
       coef[e] = (float)(of_source * weight_of(b, s, e) * b.in_counts[(size_t)s * X + e]);
@@ -503,20 +596,36 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance_grad(Balance b) {
       const int e = R::expert(lane, i);
       c[i] = e < X ? coef[e] : 0.0f;
     }
-    for (long long t = t0 + wave * kRows + slot; t < t1; t += kWaves * kRows) {
+    const auto work = [&](R& row) {
       float x[kValues];
-      R row;
-      row.load((const T*)b.logits + t * b.logits_stride, lane, X);
+      row.cut(lane, X);
       const float sum = row.exponentials(x);
       float dot = 0.0f;
 #pragma unroll
       for (int i = 0; i < kValues; ++i) dot = __builtin_fmaf(x[i], c[i], dot);
       dot = over_lanes<kLanes>(dot, [](float a, float b) { return a + b; });
-      const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+      const float inv = sum != 0.0f ? __builtin_amdgcn_rcpf(sum) : 0.0f;
       dot *= inv;
+      R z;
 #pragma unroll
-      for (int i = 0; i < kValues; ++i) row.set(i, x[i] * inv * (c[i] - dot));
-      row.store((T*)b.grad + t * b.grad_stride, lane, X);
+      for (int i = 0; i < kValues; ++i) z.set(i, x[i] * inv * (c[i] - dot));
+      z.store(to, lane, X);
+      to += grad_step;
+      left -= kStep;
+    };
+    while (left > 0) {
+      next();
+      if constexpr (row_ahead(kValues)) {
+        rows_of[1].load(at, lane, X);
+        work(rows_of[0]);
+        if (left <= 0) break;
+        next();
+        rows_of[0].load(at, lane, X);
+        work(rows_of[1]);
+      } else {
+        work(rows_of[0]);
+        rows_of[0].load(at, lane, X);
+      }
     }
     __syncthreads();
   });

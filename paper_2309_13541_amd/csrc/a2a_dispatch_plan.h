@@ -100,8 +100,24 @@ struct BalanceCut {
 };
 inline BalanceCut balance_cut(int64_t tokens) {
   BalanceCut c;
-  c.per = std::max<int64_t>(64, (tokens + 2047) / 2048);
+  c.per = std::max<int64_t>({16, (tokens + 1535) / 1536, std::min<int64_t>(256, (tokens + 511) / 512)});
   c.groups = (tokens + c.per - 1) / c.per;
+  return c;
+}
+
+// Sums over a source's pieces: about four of them for a thread.
+constexpr int kSourceGroups = 1024;  // workgroups at the most
+struct SourceCut {
+  int across = 1;
+  int groups = 1;
+};
+inline SourceCut source_cut(int64_t sources, int64_t tokens, int64_t experts) {
+  SourceCut c;
+  const int64_t pieces = sources > 0 ? balance_cut(tokens).groups / sources + 1 : 1;
+  while (c.across < 64 && pieces > 4 * c.across) c.across *= 2;
+  const int64_t each = kBalanceThreads / c.across;
+  const int64_t items = c.across > 1 ? sources * ((experts + each - 1) / each) : (sources * experts + each - 1) / each;
+  c.groups = (int)std::max<int64_t>(1, std::min<int64_t>(kSourceGroups, items));
   return c;
 }
 struct BalanceLayout {
@@ -119,7 +135,7 @@ inline BalanceLayout balance_layout(int64_t src_count, int64_t tokens, int64_t e
   l.sums = part((size_t)places * experts * 4);
   l.counts = part((size_t)places * experts * 4);
   l.rows = part((size_t)places * 4);
-  l.terms = part((size_t)src_count * 8);
+  l.terms = part((size_t)source_cut(src_count, tokens, experts).groups * 16);
   l.total = off;
   return l;
 }

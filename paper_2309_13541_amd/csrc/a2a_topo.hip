@@ -1273,26 +1273,33 @@ int dispatch(const a2a_topo* t, int32_t src_count, const a2a_routing* routing, i
   return A2A_OK;
 }
 
-// f(kLanes, kValues), constants, that hold `experts` numbers (a2a_dispatch_kernels.h).
+// f(a row's shape) for `experts` numbers: a shape that holds them with four fifths of its places used or more, from 128
+// numbers on; pieces of 16 bytes (wide) or single numbers.
+template <bool kWide_, int kLanes_, int kValues_>
+struct RowShape {
+  static constexpr bool kWide = kWide_;
+  static constexpr int kLanes = kLanes_, kValues = kValues_;
+};
 template <typename F>
 void by_row(int experts, bool wide, F&& f) {
-  const auto call = [&](auto lanes, auto values) { f(lanes, values); };
-  using std::integral_constant;
   if (!wide) {
-    if (experts <= 16 * 8) call(integral_constant<int, 16>{}, integral_constant<int, 8>{});
-    else if (experts <= 16 * 32) call(integral_constant<int, 16>{}, integral_constant<int, 32>{});
-    else call(integral_constant<int, 64>{}, integral_constant<int, 64>{});
-    return;
+    if (experts <= 128) return f(RowShape<false, 16, 8>{});
+    if (experts <= 512) return f(RowShape<false, 16, 32>{});
+    return f(RowShape<false, 64, 64>{});
   }
-  if (experts <= 8) call(integral_constant<int, 1>{}, integral_constant<int, 8>{});
-  else if (experts <= 16) call(integral_constant<int, 2>{}, integral_constant<int, 8>{});
-  else if (experts <= 32) call(integral_constant<int, 4>{}, integral_constant<int, 8>{});
-  else if (experts <= 64) call(integral_constant<int, 8>{}, integral_constant<int, 8>{});
-  else if (experts <= 128) call(integral_constant<int, 16>{}, integral_constant<int, 8>{});
-  else if (experts <= 256) call(integral_constant<int, 16>{}, integral_constant<int, 16>{});
-  else if (experts <= 512) call(integral_constant<int, 16>{}, integral_constant<int, 32>{});
-  else if (experts <= 1024) call(integral_constant<int, 16>{}, integral_constant<int, 64>{});
-  else call(integral_constant<int, 64>{}, integral_constant<int, 64>{});
+  if (experts <= 8) return f(RowShape<true, 1, 8>{});
+  if (experts <= 16) return f(RowShape<true, 2, 8>{});
+  if (experts <= 32) return f(RowShape<true, 4, 8>{});
+  if (experts <= 64) return f(RowShape<true, 8, 8>{});
+  if (experts <= 128) return f(RowShape<true, 16, 8>{});
+  if (experts <= 192) return f(RowShape<true, 8, 24>{});
+  if (experts <= 256) return f(RowShape<true, 16, 16>{});
+  if (experts <= 320) return f(RowShape<true, 8, 40>{});
+  if (experts <= 384) return f(RowShape<true, 16, 24>{});
+  if (experts <= 512) return f(RowShape<true, 16, 32>{});
+  if (experts <= 640) return f(RowShape<true, 16, 40>{});
+  if (experts <= 1024) return f(RowShape<true, 16, 64>{});
+  f(RowShape<true, 64, 64>{});
 }
 
 // f(x), x a number of the type
@@ -1305,30 +1312,35 @@ void by_float(int type, F&& f) {
   }
 }
 
-bool rows_of_pieces(const void* p, int64_t stride, size_t bytes) { return aligned_to(p, 16) && stride * bytes % 16 == 0; }
+bool rows_of_pieces(const void* p, int64_t stride, int experts, size_t bytes) {
+  return aligned_to(p, 16) && stride * bytes % 16 == 0 && experts * bytes % 16 == 0;
+}
 
 int balance_loss(const a2a_topo* t, const a2a_routing* routing, int type, Balance& b, hipStream_t st) {
   const Use use(t, st);
   ProfScope ps(t, PROF_TOKENS, st);
   const BalanceCut cut = balance_cut(b.r.tokens);
   b.per = cut.per;
-  if (cut.groups > 0 && b.r.sources > 0) {
-    const bool wide = rows_of_pieces(b.logits, b.logits_stride, type_bytes(type));
-    const size_t lds = ((size_t)(kBalanceThreads / kWave + 1) * b.r.experts + kBalanceThreads / kWave) * 4;
-    by_float(type, [&](auto x) {
-      using T = decltype(x);
-      by_row(b.r.experts, wide, [&](auto lanes, auto values) {
-        constexpr int L = decltype(lanes)::value, V = decltype(values)::value;
-        const auto launch = [&](auto kernel) { kernel<<<(unsigned)cut.groups, kBalanceThreads, lds, st>>>(b); };
-        if (routing->choices_type == A2A_I64)
-          wide ? launch(k_balance_rows<T, true, L, V, int64_t>) : launch(k_balance_rows<T, false, L, V, int64_t>);
-        else
-          wide ? launch(k_balance_rows<T, true, L, V, int32_t>) : launch(k_balance_rows<T, false, L, V, int32_t>);
-      });
-    });
+  if (b.r.sources == 0) {  // a loss of 0 alone
+    k_fill<<<1, 1, 0, st>>>((int32_t*)b.out_loss, 1);
+    HIP_TRY(hipGetLastError());
+    return A2A_OK;
   }
-  if (b.r.sources > 0) k_balance_sources<<<(unsigned)b.r.sources, kBalanceThreads, 0, st>>>(b);
-  k_balance_loss<<<1, kBalanceThreads, 0, st>>>(b);
+  const bool wide = rows_of_pieces(b.logits, b.logits_stride, b.r.experts, type_bytes(type));
+  const size_t lds = ((size_t)(kBalanceThreads / kWave + 1) * b.r.experts + kBalanceThreads / kWave) * 4;
+  b.wide_choices = routing->choices_type == A2A_I64;
+  by_float(type, [&](auto x) {
+    using T = decltype(x);
+    by_row(b.r.experts, wide, [&](auto shape) {
+      using S = decltype(shape);
+      const auto launch = [&](auto kernel) { kernel<<<(unsigned)std::max<int64_t>(cut.groups, 1), kBalanceThreads, lds, st>>>(b); };
+      launch(k_balance_rows<T, S::kWide, S::kLanes, S::kValues>);
+    });
+  });
+  const SourceCut sources = source_cut(b.r.sources, b.r.tokens, b.r.experts);
+  b.across = sources.across;
+  k_balance_sources<<<sources.groups, kBalanceThreads, 0, st>>>(b);
+  k_balance_loss<<<1, kBalanceThreads, 0, st>>>(b, sources.groups);
   HIP_TRY(hipGetLastError());
   return A2A_OK;
 }
@@ -1340,14 +1352,14 @@ int balance_grad(const a2a_topo* t, int type, Balance& b, hipStream_t st) {
   b.per = cut.per;
   if (cut.groups == 0 || b.r.sources == 0) return A2A_OK;
   const size_t bytes = type_bytes(type);
-  const bool wide = rows_of_pieces(b.logits, b.logits_stride, bytes) && rows_of_pieces(b.grad, b.grad_stride, bytes);
+  const bool wide = rows_of_pieces(b.logits, b.logits_stride, b.r.experts, bytes) && rows_of_pieces(b.grad, b.grad_stride, b.r.experts, bytes);
   const size_t lds = (kBalanceThreads / kWave + 1) * 8 + (size_t)b.r.experts * 4;
   by_float(type, [&](auto x) {
     using T = decltype(x);
-    by_row(b.r.experts, wide, [&](auto lanes, auto values) {
-      constexpr int L = decltype(lanes)::value, V = decltype(values)::value;
+    by_row(b.r.experts, wide, [&](auto shape) {
+      using S = decltype(shape);
       const auto launch = [&](auto kernel) { kernel<<<(unsigned)cut.groups, kBalanceThreads, lds, st>>>(b); };
-      wide ? launch(k_balance_grad<T, true, L, V>) : launch(k_balance_grad<T, false, L, V>);
+      launch(k_balance_grad<T, S::kWide, S::kLanes, S::kValues>);
     });
   });
   HIP_TRY(hipGetLastError());

@@ -84,9 +84,27 @@ int main() {
       const BalanceLayout l = balance_layout(sources, tokens, 48);
       const size_t places = (size_t)(c.groups + sources);
       if (l.counts - l.sums < places * 48 * 4 || l.rows - l.counts < places * 48 * 4 || l.terms - l.rows < places * 4 ||
-          l.total - l.terms < (size_t)sources * 8 || l.total % 256 != 0) ++bad;
+          l.total - l.terms < (size_t)source_cut(sources, tokens, 48).groups * 16 || l.total % 256 != 0) ++bad;
+      for (int64_t experts : {1, 48, 300, 4096}) {
+        const SourceCut q = source_cut(sources, tokens, experts);
+        if (q.across < 1 || kBalanceThreads % q.across != 0 || q.groups < 1 || q.groups > kSourceGroups) ++bad;
+      }
     }
   }
+  // every source and row has a band or pieces, within the LDS of a workgroup; no launch is too large
+  for (int64_t sources = 1; sources <= 4194304; sources = sources * 3 / 2 + 1)
+    for (int64_t tokens = 0; tokens <= INT32_MAX / 64; tokens = tokens * 2 + 1)
+      for (int64_t k : {1, 2, 8, 64})
+        for (int64_t rows : {1, 63, 4096, 4097, 65536, 70001})
+          for (bool demand : {false, true}) {
+            const DispatchCut c = dispatch_cut(sources, tokens, k, rows, demand);
+            const int64_t bands = (sources + c.columns - 1) / c.columns;
+            if (c.tile < 1 || (int64_t)c.tile * c.tiles < rows || c.columns > kDispatchColumns || (!demand && c.columns != 1) || c.lds > 131328 ||
+                c.threads > kDispatchThreads || c.threads % 64 != 0) ++bad;
+            if (c.split ? c.per < 1 || c.lds < (size_t)c.tile * 4 || c.groups / c.tiles * c.per < tokens || c.groups % c.tiles != 0
+                        : c.groups != bands * c.tiles || c.lds * 2 < (size_t)c.tile * c.columns * 4) ++bad;
+            if (sources * rows < 1ll << 33 && c.groups * c.threads > 0xffffffffll) ++bad;
+          }
   std::printf("%d bad\n", bad);
   return bad != 0;
 }
