@@ -101,8 +101,10 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_sources(CostView c) {
 #pragma unroll
           for (int j = 0; j < KS; ++j) q[j] = p[j];
 #pragma unroll
-          for (int j = 0; j < 2 * KS; ++j)
-            if (mask >> j & 1u) b[i] = __builtin_fma(value[r.template at<0>(j) >> kShift], j & 1 ? q[j / 2].y : q[j / 2].x, b[i]);
+          for (int j = 0; j < 2 * KS; ++j) {
+            const double paths = value[r.template at<0>(j) >> kShift];
+            b[i] = __builtin_fma(mask >> j & 1u ? paths : 0.0, j & 1 ? q[j / 2].y : q[j / 2].x, b[i]);
+          }
         } else {
           b[i] = value[v];
         }
@@ -148,10 +150,12 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_sources(CostView c) {
     __syncthreads();
     const auto at = [&](uint32_t id) -> double& { return value[id >> kShift]; };
     const auto add = [&](uint32_t w, const SmallRow<KS>& r) {
-      double x = at(w & 0xffffu);
+      // all in flight together: one by one, where there is a last link, each would wait for the one before
+      double x = at(w & 0xffffu), y[2 * KS];
 #pragma unroll
-      for (int j = 0; j < 2 * KS; ++j)
-        if (w >> (16 + j) & 1u) x += at(r.template at<0>(j));
+      for (int j = 0; j < 2 * KS; ++j) y[j] = at(r.template at<0>(j));
+#pragma unroll
+      for (int j = 0; j < 2 * KS; ++j) x += w >> (16 + j) & 1u ? y[j] : 0.0;
       at(w & 0xffffu) = x;
     };
     const auto fetch = [&](int i, uint32_t& w, SmallRow<KS>& r) {
@@ -191,27 +195,167 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_sources(CostView c) {
   }
 }
 
-// A workgroup per source, every level a pass over the level bytes of all nodes in LDS; a wave without a node of the level
-// goes on.  Costs lie in LDS (kCostsInLds) or where they go.  The mean over the last links wants path counts only where
-// there are several.
-template <int KS, bool kCostsInLds>
+static __device__ const double kCostUnit = 1.0;  // of a link, where the call has no link costs
+
+// Mean over the last links of a node's shortest paths, those that `mask` says, with everything that it takes in flight together:
+// a place without such a link asks for what the node itself has.
+template <int KS>
+__device__ __forceinline__ double cost_mean(const CostView& c, const double* value, const double* sigma, const SmallRow<KS>& r,
+                                            uint32_t mask, int v) {
+  constexpr int kHalf = KS <= 4 ? 2 * KS : KS;  // as many at a time as there are registers for
+  const double* const price = c.prices + (size_t)v * (2 * KS);
+  double sum = 0.0, paths = 0.0;
+#pragma unroll
+  for (int j0 = 0; j0 < 2 * KS; j0 += kHalf) {
+    double n[kHalf], x[kHalf], w[kHalf];
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j) {
+      const uint32_t u = mask >> (j0 + j) & 1u ? r.template at<0>(j0 + j) : (uint32_t)v;
+      n[j] = sigma[u];
+      x[j] = value[u];
+    }
+    if (c.link_cost != nullptr) {
+#pragma unroll
+      for (int j = 0; j < kHalf; j += 2) {
+        const double2 p = *(const double2*)(price + j0 + j);
+        w[j] = p.x;
+        w[j + 1] = p.y;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kHalf; ++j) w[j] = 1.0;
+    }
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j) {
+      const bool on = mask >> (j0 + j) & 1u;  // (the node has no cost yet: what is there may be no number)
+      sum = __builtin_fma(on ? n[j] : 0.0, on ? x[j] + w[j] : 0.0, sum);
+      paths += on ? n[j] : 0.0;
+    }
+  }
+  return sum / paths;
+}
+
+template <int KS>
+__device__ __forceinline__ uint32_t last_links(const SmallRow<KS>& r, const unsigned char* level, int l) {
+  uint32_t mask = 0;
+#pragma unroll
+  for (int j = 0; j < 2 * KS; ++j) mask |= (level[r.template at<0>(j)] + 1 == l ? 1u : 0u) << j;
+  return mask;
+}
+
+// The link of `mask`, or the first, and where it starts.
+template <int KS>
+__device__ __forceinline__ void only_link(const SmallRow<KS>& r, uint32_t mask, int& place, uint32_t& from) {
+  place = mask != 0 ? __builtin_ctz(mask) : 0;
+  from = r.template at<0>(0);
+#pragma unroll
+  for (int j = 1; j < 2 * KS; ++j) from = place == j ? r.template at<0>(j) : from;
+}
+
+// A workgroup per source, level bytes and costs in LDS, every level a pass over a thread's nodes; a wave without a node of
+// the level goes on.  What a node needs whose shortest paths have one last link, its start and its cost, is found for all
+// nodes at once before; path counts are wanted only where there are several.  The next source's distances are under way
+// meanwhile.
+template <int KS>
 __global__ void __launch_bounds__(kCostThreads) k_cost_scan(CostView c) {
+  constexpr int kNodes = kCostScanNodes, kAhead = KS <= 4 ? 4 : 1;
+  constexpr uint32_t kSeveral = 1u << 31;
   extern __shared__ __align__(16) unsigned char cost_state[];
-  const int N = c.N, pad = (N + 15) / 16 * 16;
-  unsigned char* const level = cost_state + (kCostsInLds ? 8 * pad : 0);
+  const int N = c.N;
+  double* const value = (double*)cost_state;
+  unsigned char* const level = cost_state + 8 * ((N + 15) / 16 * 16);
   const bool priced = c.link_cost != nullptr;
+  int dist[kNodes];
+  const auto ask = [&](int s, int tid) {
+#pragma unroll
+    for (int i = 0; i < kNodes; ++i) dist[i] = (c.dist + (size_t)s * N)[(uint32_t)min(tid + i * kCostThreads, N - 1)];
+  };
+  ask(blockIdx.x, threadIdx.x);
   for (int s = blockIdx.x; s < c.sources; s += gridDim.x) {
     const size_t row = (size_t)s * N;
-    double* const value = kCostsInLds ? (double*)cost_state : c.cost + row;
-    const double* const sigma = c.sigma + row;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    uint32_t levels[kNodes / 4] = {};
+#pragma unroll
+    for (int i = 0; i < kNodes; ++i) {
+      const int v = tid + i * kCostThreads;
+      const int l = v < N && (unsigned)dist[i] <= (unsigned)c.depth ? dist[i] : kSmallUnseen;
+      levels[i / 4] |= (uint32_t)l << (i % 4 * 8);
+      if (v < N) {
+        level[v] = (unsigned char)l;
+        if (l == 0 || l == kSmallUnseen) {
+          value[v] = 0.0;
+          (c.cost + row)[(uint32_t)v] = 0.0;
+        }
+      }
+    }
+    __syncthreads();
+    uint32_t from[kNodes];
+    double price[kNodes];
+#pragma unroll
+    for (int i0 = 0; i0 < kNodes; i0 += kAhead) {
+      asm volatile("" : "+v"(tid));
+      SmallRow<KS> r[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) r[i].load(c.in, 8 * min(tid + (i0 + i) * kCostThreads, N - 1));
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int v = min(tid + (i0 + i) * kCostThreads, N - 1);
+        const uint32_t mask = last_links(r[i], level, (int)(levels[(i0 + i) / 4] >> ((i0 + i) % 4 * 8) & 0xffu));
+        int place;
+        only_link(r[i], mask, place, from[i0 + i]);
+        if ((mask & (mask - 1)) != 0) from[i0 + i] |= kSeveral;
+        asm volatile("" : "+v"(from[i0 + i]));  // here, not where it is used: the row would have to stay
+        price[i0 + i] = *(priced ? c.prices + (uint32_t)(v * (2 * KS) + place) : &kCostUnit);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    asm volatile("" : "+v"(tid));
+    ask(min(s + (int)gridDim.x, c.sources - 1), tid);
+    for (int l = 1; l <= c.depth; ++l) {
+      asm volatile("" : "+v"(tid));  // nor are places kept from one level to the next
+      uint32_t several = 0;  // a bit for each node of the level that has several last links: a lane takes its own one by one
+#pragma unroll
+      for (int i = 0; i < kNodes; ++i) {
+        if ((levels[i / 4] >> (i % 4 * 8) & 0xffu) != (uint32_t)l) continue;
+        if (from[i] & kSeveral) {
+          several |= 1u << i;
+          continue;
+        }
+        const int v = tid + i * kCostThreads;
+        const double x = value[from[i]] + price[i];
+        value[v] = x;
+        (c.cost + row)[(uint32_t)v] = x;
+      }
+      while (several != 0) {
+        const int v = tid + __builtin_ctz(several) * kCostThreads;
+        several &= several - 1;
+        SmallRow<KS> r;
+        r.load(c.in, 8 * v);
+        const double x = cost_mean<KS>(c, value, c.sigma + row, r, last_links(r, level, l), v);
+        value[v] = x;
+        c.cost[row + v] = x;
+      }
+      lds_barrier();
+    }
+    __syncthreads();
+  }
+}
+
+// The same with costs where they go, in memory, for more nodes than LDS has doubles for.
+template <int KS>
+__global__ void __launch_bounds__(kCostThreads) k_cost_scan_memory(CostView c) {
+  extern __shared__ __align__(16) unsigned char cost_state[];
+  unsigned char* const level = cost_state;
+  const int N = c.N;
+  for (int s = blockIdx.x; s < c.sources; s += gridDim.x) {
+    const size_t row = (size_t)s * N;
+    double* const value = c.cost + row;
     for (int v = threadIdx.x; v < N; v += kCostThreads) {
       const int d = c.dist[row + v];
       const int l = (unsigned)d <= (unsigned)c.depth ? d : kSmallUnseen;
       level[v] = (unsigned char)l;
-      if (l == 0 || l == kSmallUnseen) {
-        value[v] = 0.0;
-        if (kCostsInLds) c.cost[row + v] = 0.0;
-      }
+      if (l == 0 || l == kSmallUnseen) value[v] = 0.0;
     }
     __syncthreads();
     for (int l = 1; l <= c.depth; ++l) {
@@ -219,32 +363,18 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_scan(CostView c) {
         if (level[v] != l) continue;
         SmallRow<KS> r;
         r.load(c.in, 8 * v);
-        uint32_t mask = 0;
-#pragma unroll
-        for (int j = 0; j < 2 * KS; ++j) mask |= (level[r.template at<0>(j)] + 1 == l ? 1u : 0u) << j;
-        double sum = 0.0, paths = 0.0;
-        const double* const price = c.prices + (size_t)v * (2 * KS);
+        const uint32_t mask = last_links(r, level, l);
         if ((mask & (mask - 1)) == 0) {
-#pragma unroll
-          for (int j = 0; j < 2 * KS; ++j)
-            if (mask >> j & 1u) sum = value[r.template at<0>(j)] + (priced ? price[j] : 1.0);
+          int place;
+          uint32_t from;
+          only_link(r, mask, place, from);
+          value[v] = value[from] + (c.link_cost != nullptr ? c.prices[(size_t)v * (2 * KS) + place] : 1.0);
         } else {
-#pragma unroll
-          for (int j = 0; j < 2 * KS; ++j)
-            if (mask >> j & 1u) {
-              const uint32_t u = r.template at<0>(j);
-              const double n = sigma[u];
-              sum = __builtin_fma(n, value[u] + (priced ? price[j] : 1.0), sum);
-              paths += n;
-            }
-          sum /= paths;
+          value[v] = cost_mean<KS>(c, value, c.sigma + row, r, mask, v);
         }
-        value[v] = sum;
-        if (kCostsInLds) c.cost[row + v] = sum;
       }
-      kCostsInLds ? lds_barrier() : __syncthreads();
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 

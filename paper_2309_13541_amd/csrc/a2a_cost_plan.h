@@ -8,6 +8,7 @@ namespace a2a_dev {
 
 constexpr int kCostThreads = 1024;
 constexpr int kCostDeepest = 253;   // levels are bytes, 255 is a node that is not reached, and no level is one less
+constexpr int kCostScanNodes = 16;  // nodes of a thread in k_cost_scan
 constexpr int kCostGroups = 256;    // workgroups whose lists lie in the workspace
 
 // Nodes of a thread where a source's state fits LDS (k_cost_sources); 0: it does not, or there is no link table.

@@ -1222,7 +1222,7 @@ void path_costs(const a2a_topo* t, CostView& c, char* ws, hipStream_t st) {
     k_cost_prices<<<(unsigned)((t->N * 2 * t->ell_words + kBlock - 1) / kBlock), kBlock, 0, st>>>(c);
   }
   const int nodes = way == CostWay::kSources ? cost_nodes(t->N, t->ell_words, t->level_bound) : way == CostWay::kScan ? 0 : -1;
-  const int workgroups = cost_list_in_lds(nodes) ? c.sources : std::min(c.sources, kCostGroups);
+  const int workgroups = nodes != 0 && cost_list_in_lds(nodes) ? c.sources : std::min(c.sources, kCostGroups);
   ProfScope ps(t, PROF_SOURCES, st);
   by_words(t->ell_words, [&](auto ks) { launch_cost_sources<decltype(ks)::value>(c, nodes, workgroups, st); });
 }

@@ -185,8 +185,8 @@ void launch_cost_sources(const CostView& cv, int nodes, int workgroups, hipStrea
   const auto launch = [&](auto kernel) { kernel<<<workgroups, cost_threads(cv.N, nodes), cost_lds(cv.N, nodes, cv.depth), st>>>(cv); };
   const auto scan = [&](auto kernel, bool costs) { kernel<<<workgroups, kCostThreads, cost_scan_lds(cv.N, costs), st>>>(cv); };
   switch (nodes) {
-    case 0: return scan(k_cost_scan<KS, true>, true);
-    case -1: return scan(k_cost_scan<KS, false>, false);
+    case 0: return scan(k_cost_scan<KS>, true);
+    case -1: return scan(k_cost_scan_memory<KS>, false);
     case 2: return launch(k_cost_sources<KS, 2>);
     case 8: return launch(k_cost_sources<KS, 8>);
     default: return launch(k_cost_sources<KS, 16>);
