@@ -47,8 +47,9 @@ __device__ __forceinline__ uint64_t lanes_like(unsigned x, int bits) {
 // node; the nodes in the order of levels, with a bit for each place of the link table that is a last link.  A thread has
 // kNodes nodes for what needs no order.  Places in a level are handed out a wave at a time (an atomic addition a level and
 // wave); their order changes nothing, a node's sum is its own.
+constexpr int cost_waves(int words, int nodes) { return nodes <= 4 && words <= 4 ? 8 : 4; }  // a SIMD
 template <int KS, int kNodes>
-__global__ void __launch_bounds__(kCostThreads) k_cost_sources(CostView c) {
+__global__ void __launch_bounds__(kCostThreads, cost_waves(KS, kNodes)) k_cost_sources(CostView c) {
   constexpr bool kInLds = cost_list_in_lds(kNodes);
   constexpr int kShift = kNodes < 16 ? 3 : 0;  // ids of the table are 8 x id up to kScaledNodes
   extern __shared__ __align__(16) unsigned char cost_state[];
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_sources(CostView c) {
 #pragma unroll
     for (int i = 0; i < kNodes; ++i) {
       const int v = tid + i * T;
-      if (v < N) c.cost[row + v] = level[v] - 1u < (unsigned)c.depth ? value[v] / (kKept ? sigma[i] : c.sigma[row + v]) : 0.0;
+      if (v < N) c.cost[row + v] = level[v] - 1u < (unsigned)c.depth ? value[v] * recip(kKept ? sigma[i] : c.sigma[row + v]) : 0.0;
       __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();

@@ -14,7 +14,7 @@ constexpr int kCostGroups = 256;    // workgroups whose lists lie in the workspa
 // Nodes of a thread where a source's state fits LDS (k_cost_sources); 0: it does not, or there is no link table.
 constexpr int cost_nodes(int N, int words, int depth) {
   if (words == 0 || depth > kCostDeepest) return 0;
-  return N <= 1024 ? 2 : N <= kScaledNodes ? 8 : N <= 16 * kCostThreads ? 16 : 0;
+  return N <= 1024 ? 2 : N <= 4096 ? 4 : N <= kScaledNodes ? 8 : N <= 16 * kCostThreads ? 16 : 0;
 }
 constexpr bool cost_list_in_lds(int nodes) { return nodes < 16; }
 constexpr int cost_threads(int N, int nodes) {

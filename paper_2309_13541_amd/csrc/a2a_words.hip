@@ -188,6 +188,7 @@ void launch_cost_sources(const CostView& cv, int nodes, int workgroups, hipStrea
     case 0: return scan(k_cost_scan<KS>, true);
     case -1: return scan(k_cost_scan_memory<KS>, false);
     case 2: return launch(k_cost_sources<KS, 2>);
+    case 4: return launch(k_cost_sources<KS, 4>);
     case 8: return launch(k_cost_sources<KS, 8>);
     default: return launch(k_cost_sources<KS, 16>);
   }
