@@ -20,6 +20,8 @@ struct CostView {
   const double* link_cost;
   double* prices;   // of the places of the link table, if there are link costs
   uint32_t* lists;  // [workgroups][N]
+  unsigned char* levels;  // [sources][N], with the places of the last links
+  uint16_t* masks;
   double* cost;
   int N, sources, depth, words;
 };
@@ -375,6 +377,55 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_scan_memory(CostView c) {
         }
       }
       __syncthreads();
+    }
+  }
+}
+
+// Many sources of more nodes, a launch a level.  First a byte with its level and the places of its last links for every node, a
+// workgroup per source with the level bytes in LDS; also the costs that need no link.
+template <int KS>
+__global__ void __launch_bounds__(kCostThreads) k_cost_marks(CostView c) {
+  extern __shared__ __align__(16) unsigned char cost_state[];
+  unsigned char* const level = cost_state;
+  const int N = c.N;
+  const size_t row = (size_t)blockIdx.x * N;
+  for (int v = threadIdx.x; v < N; v += kCostThreads) {
+    const int d = c.dist[row + v];
+    const int l = (unsigned)d <= (unsigned)c.depth ? d : kSmallUnseen;
+    level[v] = (unsigned char)l;
+    c.levels[row + v] = (unsigned char)l;
+    if (l == 0 || l == kSmallUnseen) c.cost[row + v] = 0.0;
+  }
+  __syncthreads();
+  for (int v = threadIdx.x; v < N; v += kCostThreads) {
+    SmallRow<KS> r;
+    r.load(c.in, 8 * v);
+    c.masks[row + v] = (uint16_t)last_links(r, level, level[v]);
+  }
+}
+
+// Then the nodes of one level.  A workgroup has kCostLevelNodes of a source; workgroups go to the 8 XCDs in turn, and those of an
+// XCD have the parts of its sources one after the other, so that the rows of costs and path counts that they gather from, 1 MB
+// a source of 65536 nodes, stay in its L2.
+template <int KS>
+__global__ void __launch_bounds__(kCostThreads) k_cost_level(CostView c, int l, int parts) {
+  const int k = blockIdx.x / kXcd, s = k / parts * kXcd + blockIdx.x % kXcd;
+  if (s >= c.sources) return;
+  const size_t row = (size_t)s * c.N;
+  double* const value = c.cost + row;
+  for (int i = 0; i < kCostLevelNodes / kCostThreads; ++i) {
+    const int v = k % parts * kCostLevelNodes + i * kCostThreads + threadIdx.x;
+    if (v >= c.N || c.levels[row + v] != l) continue;
+    const uint32_t mask = c.masks[row + v];
+    SmallRow<KS> r;
+    r.load(c.in, 8 * v);
+    if ((mask & (mask - 1)) == 0) {
+      int place;
+      uint32_t from;
+      only_link(r, mask, place, from);
+      value[v] = value[from] + (c.link_cost != nullptr ? c.prices[(size_t)v * (2 * KS) + place] : 1.0);
+    } else {
+      value[v] = cost_mean<KS>(c, value, c.sigma + row, r, mask, v);
     }
   }
 }

@@ -28,20 +28,23 @@ constexpr size_t cost_lds(int N, int nodes, int depth) {
 }
 static_assert(cost_lds(16 * kCostThreads, 16, kCostDeepest) <= kSmallLds && cost_lds(kScaledNodes, 8, kCostDeepest) <= kSmallLds);
 
-// Topologies of few levels or many nodes: k_cost_scan.
-enum class CostWay { kLevels, kSources, kScan, kScanMemory };
-constexpr CostWay cost_way(int N, int words, int depth) {
+// Topologies of few levels or many nodes: a scan of all nodes a level, of a source by a workgroup or of all sources by a launch.
+constexpr int kCostFewLevels = 16;
+constexpr int kCostLevelSources = 1024;  // at a time, at the most
+constexpr int kCostLevelNodes = 2048;
+enum class CostWay { kLevels, kSources, kScan, kScanMemory, kLevelLaunches };
+constexpr CostWay cost_way(int N, int words, int depth, int sources) {
   if (words == 0 || depth > kCostDeepest) return CostWay::kLevels;
-  if (N > kScaledNodes && N <= 16 * kCostThreads && depth <= 16) return CostWay::kScan;
+  if (N > kScaledNodes && N <= kCostScanNodes * kCostThreads && depth <= kCostFewLevels) return CostWay::kScan;
   if (cost_nodes(N, words, depth) > 0) return CostWay::kSources;
-  return CostWay::kScanMemory;
+  return depth <= kCostFewLevels && sources >= 64 ? CostWay::kLevelLaunches : CostWay::kScanMemory;
 }
 constexpr size_t cost_scan_lds(int N, bool costs) { return (size_t)(N + 15) / 16 * 16 * (costs ? 9 : 1); }
 
 struct CostLayout {
-  size_t prices = 0, lists = 0, total = 0;
+  size_t prices = 0, lists = 0, levels = 0, masks = 0, total = 0;
 };
-inline CostLayout cost_layout(int N, int words, int depth) {
+inline CostLayout cost_layout(int N, int words, int depth, int sources) {
   CostLayout l;
   size_t off = 0;
   const auto part = [&off](size_t bytes) {
@@ -49,10 +52,13 @@ inline CostLayout cost_layout(int N, int words, int depth) {
     off += (bytes + 255) / 256 * 256;
     return at;
   };
-  const CostWay way = cost_way(N, words, depth);
+  const CostWay way = cost_way(N, words, depth, sources);
   const bool lists = way == CostWay::kSources && !cost_list_in_lds(cost_nodes(N, words, depth));
+  const size_t marks = way == CostWay::kLevelLaunches ? (size_t)std::min(sources, kCostLevelSources) * N : 0;
   l.prices = part(way != CostWay::kLevels ? (size_t)N * words * 16 : 0);
   l.lists = part(lists ? (size_t)kCostGroups * N * 4 : 0);
+  l.levels = part(marks);
+  l.masks = part(marks * 2);
   l.total = off > 0 ? off : 256;
   return l;
 }

@@ -51,6 +51,10 @@ void launch_flow_links(const FlowView& fv, bool demand, hipStream_t st);
 
 template <int KS>
 void launch_cost_sources(const CostView& cv, int nodes, int workgroups, hipStream_t st);
+template <int KS>
+void launch_cost_marks(const CostView& cv, hipStream_t st);
+template <int KS>
+void launch_cost_level(const CostView& cv, int level, hipStream_t st);
 
 // f(KS), a constant, for a table of that many words a node.
 template <typename F>

@@ -1203,16 +1203,18 @@ int small_sssp(const a2a_topo* t, int32_t src_begin, int32_t src_count, int32_t 
   return A2A_OK;
 }
 
-size_t cost_workspace_bytes(const a2a_topo* t) { return cost_layout(t->N, t->ell_words, t->level_bound).total; }
+size_t cost_workspace_bytes(const a2a_topo* t, int32_t src_count) {
+  return cost_layout(t->N, t->ell_words, t->level_bound, src_count).total;
+}
 
 void path_costs(const a2a_topo* t, CostView& c, char* ws, hipStream_t st) {
-  const CostWay way = cost_way(t->N, t->ell_words, t->level_bound);
+  const CostWay way = cost_way(t->N, t->ell_words, t->level_bound, c.sources);
   if (way == CostWay::kLevels) {
     ProfScope ps(t, PROF_SOURCES, st);
     k_cost_levels<<<(unsigned)std::min(c.sources, 65535), kCostThreads, 0, st>>>(c);
     return;
   }
-  const CostLayout l = cost_layout(t->N, t->ell_words, t->level_bound);
+  const CostLayout l = cost_layout(t->N, t->ell_words, t->level_bound, c.sources);
   c.in = t->d_ell_in;
   c.prices = (double*)(ws + l.prices);
   c.lists = (uint32_t*)(ws + l.lists);
@@ -1220,6 +1222,28 @@ void path_costs(const a2a_topo* t, CostView& c, char* ws, hipStream_t st) {
   if (c.link_cost) {
     ProfScope ps(t, PROF_OFFSETS, st);
     k_cost_prices<<<(unsigned)((t->N * 2 * t->ell_words + kBlock - 1) / kBlock), kBlock, 0, st>>>(c);
+  }
+  if (way == CostWay::kLevelLaunches) {
+    c.levels = (unsigned char*)(ws + l.levels);
+    c.masks = (uint16_t*)(ws + l.masks);
+    const int sources = c.sources;
+    const CostView whole = c;
+    for (int s0 = 0; s0 < sources; s0 += kCostLevelSources) {
+      const size_t rows = (size_t)s0 * t->N;
+      c.sources = std::min(kCostLevelSources, sources - s0);
+      c.dist = whole.dist + rows;
+      c.sigma = whole.sigma + rows;
+      c.cost = whole.cost + rows;
+      {
+        ProfScope ps(t, PROF_OFFSETS, st);
+        by_words(t->ell_words, [&](auto ks) { launch_cost_marks<decltype(ks)::value>(c, st); });
+      }
+      for (int level = 1; level <= c.depth; ++level) {
+        ProfScope ps(t, PROF_SOURCES, st, level);
+        by_words(t->ell_words, [&](auto ks) { launch_cost_level<decltype(ks)::value>(c, level, st); });
+      }
+    }
+    return;
   }
   const int nodes = way == CostWay::kSources ? cost_nodes(t->N, t->ell_words, t->level_bound) : way == CostWay::kScan ? 0 : -1;
   const int workgroups = nodes != 0 && cost_list_in_lds(nodes) ? c.sources : std::min(c.sources, kCostGroups);
@@ -1518,7 +1542,7 @@ int a2a_topo_info(const a2a_topo* t, int32_t* N, int64_t* E, int32_t* dmax, int3
 size_t a2a_workspace_bytes(const a2a_topo* t, int32_t src_count, int flags) {
   if (!t || src_count < 0 || (size_t)src_count > align_up((size_t)t->N, 64)) return 0;
   if (src_count == 0) return 256;
-  if (flags & A2A_WS_COSTS) return cost_workspace_bytes(t);
+  if (flags & A2A_WS_COSTS) return cost_workspace_bytes(t, src_count);
   const bool minimal = (flags & A2A_WS_MINIMAL) != 0;
   const Layout L = make_layout(t, src_count, flags & 0xff, 0, true, minimal);
   return minimal || !(flags & A2A_WS_LOADS) || !t->small_loads ? L.total : std::max(L.total, small_loads_bytes(t, src_count));
@@ -1792,7 +1816,7 @@ int a2a_path_costs(const a2a_topo* t, int32_t src_begin, int32_t src_count, cons
   if (!dist || !sigma || !cost || !aligned_to(dist, 4) || !aligned_to(sigma, 8) || !aligned_to(cost, 8) || !aligned_to(link_cost, 8) ||
       !on_device(t))
     return A2A_ERR_INVALID_ARG;
-  if (workspace_bytes < cost_workspace_bytes(t)) return A2A_ERR_WORKSPACE_TOO_SMALL;
+  if (workspace_bytes < cost_workspace_bytes(t, src_count)) return A2A_ERR_WORKSPACE_TOO_SMALL;
   hipStream_t st = (hipStream_t)hip_stream;
   const Use use(t, st);
   CostView c{};

@@ -194,6 +194,17 @@ void launch_cost_sources(const CostView& cv, int nodes, int workgroups, hipStrea
   }
 }
 
+template <int KS>
+void launch_cost_marks(const CostView& cv, hipStream_t st) {
+  k_cost_marks<KS><<<cv.sources, kCostThreads, cost_scan_lds(cv.N, false), st>>>(cv);
+}
+
+template <int KS>
+void launch_cost_level(const CostView& cv, int level, hipStream_t st) {
+  const int parts = (cv.N + kCostLevelNodes - 1) / kCostLevelNodes;
+  k_cost_level<KS><<<(cv.sources + kXcd - 1) / kXcd * kXcd * parts, kCostThreads, 0, st>>>(cv, level, parts);
+}
+
 template void launch_small_loads<A2A_WORDS>(const SmallPlan&, bool, int, hipStream_t);
 template void launch_node_loads<A2A_WORDS>(const SmallPlan&, bool, int, hipStream_t);
 template void launch_small_outputs<A2A_WORDS>(const SmallPlan&, const SmallOut&, int, hipStream_t);
@@ -208,5 +219,7 @@ template void launch_flow_sources<A2A_WORDS>(const FlowView&, bool, int, hipStre
 template void launch_strip_sources<A2A_WORDS>(const FlowView&, int, hipStream_t);
 template void launch_flow_links<A2A_WORDS>(const FlowView&, bool, hipStream_t);
 template void launch_cost_sources<A2A_WORDS>(const CostView&, int, int, hipStream_t);
+template void launch_cost_marks<A2A_WORDS>(const CostView&, hipStream_t);
+template void launch_cost_level<A2A_WORDS>(const CostView&, int, hipStream_t);
 
 }  // namespace a2a_dev
