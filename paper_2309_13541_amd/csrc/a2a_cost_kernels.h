@@ -18,20 +18,28 @@ struct CostView {
   const int32_t* dist;
   const double* sigma;
   const double* link_cost;
-  double* prices;   // of the places of the link table, if there are link costs
+  double* prices;   // [words of the link table][N][2], if there are link costs: those of a wave's nodes lie next to each other
   uint32_t* lists;  // [workgroups][N]
   unsigned char* levels;  // [sources][N], with the places of the last links
   uint16_t* masks;
+  double2* pairs;  // [sources][N] path count and cost
   double* cost;
   int N, sources, depth, words;
 };
+
+// Element i of an array at a uniform address, by a 32-bit offset of bytes: no 64-bit addition a lane.
+template <typename T>
+__device__ __forceinline__ T& near(T* base, int i) {
+  return *reinterpret_cast<T*>(reinterpret_cast<char*>(const_cast<std::remove_const_t<T>*>(base)) + (uint32_t)(i * (int)sizeof(T)));
+}
+__device__ __forceinline__ int price_at(int place, int v, int N) { return (place / 2 * N + v) * 2 + place % 2; }
 
 // Link costs by place of the link table.
 static __global__ void __launch_bounds__(kBlock) k_cost_prices(CostView c) {
   const int places = 2 * c.words;
   const int i = blockIdx.x * kBlock + threadIdx.x;
   if (i >= c.N * places) return;
-  const int v = i / places, p = c.in_ptr[v] + (i - v * places);
+  const int q = i / 2 / c.N, v = i / 2 - q * c.N, p = c.in_ptr[v] + 2 * q + i % 2;
   c.prices[i] = p < c.in_ptr[v + 1] ? c.link_cost[c.in_link[p]] : 0.0;
 }
 
@@ -72,10 +80,10 @@ __global__ void __launch_bounds__(kCostThreads, cost_waves(KS, kNodes)) k_cost_s
 #pragma unroll
     for (int i = 0; i < kNodes; ++i) {
       const int v = tid + i * T;
-      sigma[i] = v < N ? c.sigma[row + v] : 0.0;
+      sigma[i] = v < N ? near(c.sigma + row, v) : 0.0;
     }
     for (int v = tid; v < N; v += T) {
-      const int d = c.dist[row + v];
+      const int d = near(c.dist + row, v);
       level[v] = (unsigned char)((unsigned)d <= (unsigned)c.depth ? d : kSmallUnseen);
     }
 #pragma unroll
@@ -99,10 +107,9 @@ __global__ void __launch_bounds__(kCostThreads, cost_waves(KS, kNodes)) k_cost_s
 #pragma unroll
         for (int j = 0; j < 2 * KS; ++j) mask |= (level[r.template at<0>(j) >> kShift] + 1 == l ? 1u : 0u) << j;
         if (priced) {
-          const double2* const p = (const double2*)(c.prices + (size_t)v * (2 * KS));
           double2 q[KS];
 #pragma unroll
-          for (int j = 0; j < KS; ++j) q[j] = p[j];
+          for (int j = 0; j < KS; ++j) q[j] = near((const double2*)c.prices, j * N + v);
 #pragma unroll
           for (int j = 0; j < 2 * KS; ++j) {
             const double paths = value[r.template at<0>(j) >> kShift];
@@ -191,7 +198,7 @@ __global__ void __launch_bounds__(kCostThreads, cost_waves(KS, kNodes)) k_cost_s
 #pragma unroll
     for (int i = 0; i < kNodes; ++i) {
       const int v = tid + i * T;
-      if (v < N) c.cost[row + v] = level[v] - 1u < (unsigned)c.depth ? value[v] * recip(kKept ? sigma[i] : c.sigma[row + v]) : 0.0;
+      if (v < N) near(c.cost + row, v) = level[v] - 1u < (unsigned)c.depth ? value[v] * recip(kKept ? sigma[i] : near(c.sigma + row, v)) : 0.0;
       __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
@@ -201,26 +208,26 @@ __global__ void __launch_bounds__(kCostThreads, cost_waves(KS, kNodes)) k_cost_s
 static __device__ const double kCostUnit = 1.0;  // of a link, where the call has no link costs
 
 // Mean over the last links of a node's shortest paths, those that `mask` says, with everything that it takes in flight together:
-// a place without such a link asks for what the node itself has.
-template <int KS>
-__device__ __forceinline__ double cost_mean(const CostView& c, const double* value, const double* sigma, const SmallRow<KS>& r,
-                                            uint32_t mask, int v) {
-  constexpr int kHalf = KS <= 4 ? 2 * KS : KS;  // as many at a time as there are registers for
-  const double* const price = c.prices + (size_t)v * (2 * KS);
+// a place without such a link asks for what node 0 has.  (64 lanes with different lines take a request 64 cycles: those that ask for
+// the same one, and prices next to each other, spare most of them.)
+// of(u): path count and cost of node u.
+template <int KS, typename F>
+__device__ __forceinline__ double cost_mean(const CostView& c, F&& of, const SmallRow<KS>& r, uint32_t mask, int v) {
+  constexpr int kHalf = KS <= 5 ? 2 * KS : KS;  // as many at a time as there are registers for
+  static_assert(kHalf % 2 == 0 && 2 * KS % kHalf == 0, "prices come in pairs");
   double sum = 0.0, paths = 0.0;
 #pragma unroll
   for (int j0 = 0; j0 < 2 * KS; j0 += kHalf) {
-    double n[kHalf], x[kHalf], w[kHalf];
+    double2 n[kHalf];
+    double w[kHalf];
 #pragma unroll
     for (int j = 0; j < kHalf; ++j) {
-      const uint32_t u = mask >> (j0 + j) & 1u ? r.template at<0>(j0 + j) : (uint32_t)v;
-      n[j] = sigma[u];
-      x[j] = value[u];
+      n[j] = of(mask >> (j0 + j) & 1u ? r.template at<0>(j0 + j) : 0u);
     }
     if (c.link_cost != nullptr) {
 #pragma unroll
       for (int j = 0; j < kHalf; j += 2) {
-        const double2 p = *(const double2*)(price + j0 + j);
+        const double2 p = near((const double2*)c.prices, (j0 + j) / 2 * c.N + v);
         w[j] = p.x;
         w[j + 1] = p.y;
       }
@@ -231,8 +238,8 @@ __device__ __forceinline__ double cost_mean(const CostView& c, const double* val
 #pragma unroll
     for (int j = 0; j < kHalf; ++j) {
       const bool on = mask >> (j0 + j) & 1u;  // (the node has no cost yet: what is there may be no number)
-      sum = __builtin_fma(on ? n[j] : 0.0, on ? x[j] + w[j] : 0.0, sum);
-      paths += on ? n[j] : 0.0;
+      sum = __builtin_fma(on ? n[j].x : 0.0, on ? n[j].y + w[j] : 0.0, sum);
+      paths += on ? n[j].x : 0.0;
     }
   }
   return sum / paths;
@@ -271,7 +278,7 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_scan(CostView c) {
   int dist[kNodes];
   const auto ask = [&](int s, int tid) {
 #pragma unroll
-    for (int i = 0; i < kNodes; ++i) dist[i] = (c.dist + (size_t)s * N)[(uint32_t)min(tid + i * kCostThreads, N - 1)];
+    for (int i = 0; i < kNodes; ++i) dist[i] = near(c.dist + (size_t)s * N, min(tid + i * kCostThreads, N - 1));
   };
   ask(blockIdx.x, threadIdx.x);
   for (int s = blockIdx.x; s < c.sources; s += gridDim.x) {
@@ -288,7 +295,7 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_scan(CostView c) {
         level[v] = (unsigned char)l;
         if (l == 0 || l == kSmallUnseen) {
           value[v] = 0.0;
-          (c.cost + row)[(uint32_t)v] = 0.0;
+          near(c.cost + row, v) = 0.0;
         }
       }
     }
@@ -309,12 +316,14 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_scan(CostView c) {
         only_link(r[i], mask, place, from[i0 + i]);
         if ((mask & (mask - 1)) != 0) from[i0 + i] |= kSeveral;
         asm volatile("" : "+v"(from[i0 + i]));  // here, not where it is used: the row would have to stay
-        price[i0 + i] = *(priced ? c.prices + (uint32_t)(v * (2 * KS) + place) : &kCostUnit);
+        price[i0 + i] = *(priced ? c.prices + price_at(place, v, N) : &kCostUnit);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
     asm volatile("" : "+v"(tid));
     ask(min(s + (int)gridDim.x, c.sources - 1), tid);
+    const double* const sigma = c.sigma + row;
+    const auto of = [&](uint32_t u) { return make_double2(sigma[u], value[u]); };
     for (int l = 1; l <= c.depth; ++l) {
       asm volatile("" : "+v"(tid));  // nor are places kept from one level to the next
       uint32_t several = 0;  // a bit for each node of the level that has several last links: a lane takes its own one by one
@@ -328,14 +337,14 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_scan(CostView c) {
         const int v = tid + i * kCostThreads;
         const double x = value[from[i]] + price[i];
         value[v] = x;
-        (c.cost + row)[(uint32_t)v] = x;
+        near(c.cost + row, v) = x;
       }
       while (several != 0) {
         const int v = tid + __builtin_ctz(several) * kCostThreads;
         several &= several - 1;
         SmallRow<KS> r;
         r.load(c.in, 8 * v);
-        const double x = cost_mean<KS>(c, value, c.sigma + row, r, last_links(r, level, l), v);
+        const double x = cost_mean<KS>(c, of, r, last_links(r, level, l), v);
         value[v] = x;
         c.cost[row + v] = x;
       }
@@ -354,6 +363,8 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_scan_memory(CostView c) {
   for (int s = blockIdx.x; s < c.sources; s += gridDim.x) {
     const size_t row = (size_t)s * N;
     double* const value = c.cost + row;
+    const double* const sigma = c.sigma + row;
+    const auto of = [&](uint32_t u) { return make_double2(sigma[u], value[u]); };
     for (int v = threadIdx.x; v < N; v += kCostThreads) {
       const int d = c.dist[row + v];
       const int l = (unsigned)d <= (unsigned)c.depth ? d : kSmallUnseen;
@@ -371,9 +382,9 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_scan_memory(CostView c) {
           int place;
           uint32_t from;
           only_link(r, mask, place, from);
-          value[v] = value[from] + (c.link_cost != nullptr ? c.prices[(size_t)v * (2 * KS) + place] : 1.0);
+          value[v] = value[from] + (c.link_cost != nullptr ? near(c.prices, price_at(place, v, N)) : 1.0);
         } else {
-          value[v] = cost_mean<KS>(c, value, c.sigma + row, r, mask, v);
+          value[v] = cost_mean<KS>(c, of, r, mask, v);
         }
       }
       __syncthreads();
@@ -395,6 +406,7 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_marks(CostView c) {
     level[v] = (unsigned char)l;
     c.levels[row + v] = (unsigned char)l;
     if (l == 0 || l == kSmallUnseen) c.cost[row + v] = 0.0;
+    if (l == 0) c.pairs[row + v] = make_double2(c.sigma[row + v], 0.0);
   }
   __syncthreads();
   for (int v = threadIdx.x; v < N; v += kCostThreads) {
@@ -405,28 +417,33 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_marks(CostView c) {
 }
 
 // Then the nodes of one level.  A workgroup has kCostLevelNodes of a source; workgroups go to the 8 XCDs in turn, and those of an
-// XCD have the parts of its sources one after the other, so that the rows of costs and path counts that they gather from, 1 MB
-// a source of 65536 nodes, stay in its L2.
+// XCD have the parts of its sources one after the other, so that the path counts and costs that they gather, 1 MB a source of
+// 65536 nodes, stay in its L2; the two lie beside each other, one request for both.
 template <int KS>
-__global__ void __launch_bounds__(kCostThreads) k_cost_level(CostView c, int l, int parts) {
+__global__ void __launch_bounds__(kCostLevelThreads) k_cost_level(CostView c, int l, int parts) {
   const int k = blockIdx.x / kXcd, s = k / parts * kXcd + blockIdx.x % kXcd;
   if (s >= c.sources) return;
   const size_t row = (size_t)s * c.N;
-  double* const value = c.cost + row;
-  for (int i = 0; i < kCostLevelNodes / kCostThreads; ++i) {
-    const int v = k % parts * kCostLevelNodes + i * kCostThreads + threadIdx.x;
+  double2* const pairs = c.pairs + row;
+  const auto of = [&](uint32_t u) { return pairs[u]; };
+  for (int i = 0; i < kCostLevelNodes / kCostLevelThreads; ++i) {
+    const int v = k % parts * kCostLevelNodes + i * kCostLevelThreads + threadIdx.x;
     if (v >= c.N || c.levels[row + v] != l) continue;
     const uint32_t mask = c.masks[row + v];
+    const double paths = c.sigma[row + v];
     SmallRow<KS> r;
     r.load(c.in, 8 * v);
+    double x;
     if ((mask & (mask - 1)) == 0) {
       int place;
       uint32_t from;
       only_link(r, mask, place, from);
-      value[v] = value[from] + (c.link_cost != nullptr ? c.prices[(size_t)v * (2 * KS) + place] : 1.0);
+      x = pairs[from].y + (c.link_cost != nullptr ? near(c.prices, price_at(place, v, c.N)) : 1.0);
     } else {
-      value[v] = cost_mean<KS>(c, value, c.sigma + row, r, mask, v);
+      x = cost_mean<KS>(c, of, r, mask, v);
     }
+    pairs[v] = make_double2(paths, x);
+    c.cost[row + v] = x;
   }
 }
 

@@ -30,8 +30,8 @@ static_assert(cost_lds(16 * kCostThreads, 16, kCostDeepest) <= kSmallLds && cost
 
 // Topologies of few levels or many nodes: a scan of all nodes a level, of a source by a workgroup or of all sources by a launch.
 constexpr int kCostFewLevels = 16;
-constexpr int kCostLevelSources = 1024;  // at a time, at the most
-constexpr int kCostLevelNodes = 2048;
+constexpr int kCostLevelSources = 512;  // at a time, at the most
+constexpr int kCostLevelThreads = 256, kCostLevelNodes = 1024;  // of a workgroup
 enum class CostWay { kLevels, kSources, kScan, kScanMemory, kLevelLaunches };
 constexpr CostWay cost_way(int N, int words, int depth, int sources) {
   if (words == 0 || depth > kCostDeepest) return CostWay::kLevels;
@@ -42,7 +42,7 @@ constexpr CostWay cost_way(int N, int words, int depth, int sources) {
 constexpr size_t cost_scan_lds(int N, bool costs) { return (size_t)(N + 15) / 16 * 16 * (costs ? 9 : 1); }
 
 struct CostLayout {
-  size_t prices = 0, lists = 0, levels = 0, masks = 0, total = 0;
+  size_t prices = 0, lists = 0, levels = 0, masks = 0, pairs = 0, total = 0;
 };
 inline CostLayout cost_layout(int N, int words, int depth, int sources) {
   CostLayout l;
@@ -59,6 +59,7 @@ inline CostLayout cost_layout(int N, int words, int depth, int sources) {
   l.lists = part(lists ? (size_t)kCostGroups * N * 4 : 0);
   l.levels = part(marks);
   l.masks = part(marks * 2);
+  l.pairs = part(marks * 16);
   l.total = off > 0 ? off : 256;
   return l;
 }

@@ -1226,6 +1226,7 @@ void path_costs(const a2a_topo* t, CostView& c, char* ws, hipStream_t st) {
   if (way == CostWay::kLevelLaunches) {
     c.levels = (unsigned char*)(ws + l.levels);
     c.masks = (uint16_t*)(ws + l.masks);
+    c.pairs = (double2*)(ws + l.pairs);
     const int sources = c.sources;
     const CostView whole = c;
     for (int s0 = 0; s0 < sources; s0 += kCostLevelSources) {

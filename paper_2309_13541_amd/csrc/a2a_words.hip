@@ -202,7 +202,7 @@ void launch_cost_marks(const CostView& cv, hipStream_t st) {
 template <int KS>
 void launch_cost_level(const CostView& cv, int level, hipStream_t st) {
   const int parts = (cv.N + kCostLevelNodes - 1) / kCostLevelNodes;
-  k_cost_level<KS><<<(cv.sources + kXcd - 1) / kXcd * kXcd * parts, kCostThreads, 0, st>>>(cv, level, parts);
+  k_cost_level<KS><<<(cv.sources + kXcd - 1) / kXcd * kXcd * parts, kCostLevelThreads, 0, st>>>(cv, level, parts);
 }
 
 template void launch_small_loads<A2A_WORDS>(const SmallPlan&, bool, int, hipStream_t);

@@ -123,7 +123,10 @@ def by_levels(rp, col, dist, sigma, w):
                                    ("random", 17000, 4, 16900, 100), ("random", 20011, 5, 7, 65), ("random", 65536, 8, 65500, 36),
                                    ("random", 65537, 3, 0, 20), ("random", 70001, 2, 70000, 1), ("random", 600, 17, 0, 600),
                                    ("random", 9001, 20, 500, 40), ("torus", (13, 17, 19), 0, 1000, 300), ("torus", (90, 90), 0, 0, 70),
-                                   ("torus", (2, 5000), 0, 77, 9), ("torus", (40, 41, 42), 0, 500, 20)], ids=str)
+                                   ("torus", (2, 5000), 0, 77, 9), ("torus", (40, 41, 42), 0, 500, 20),
+                                   ("random", 9000, 10, 0, 100), ("random", 9000, 16, 8900, 64), ("random", 17000, 10, 0, 70),
+                                   ("random", 17000, 12, 5, 80), ("random", 16385, 6, 16000, 385), ("random", 40000, 3, 39000, 700),
+                                   ("torus", (128, 128), 0, 0, 40), ("torus", (8, 8, 8, 8), 0, 0, 4096)], ids=str)
 def test_larger(a2a, shape):
     """Of every size of a topology's state, a range of sources; against the definition on the device."""
     import torch
