@@ -218,7 +218,8 @@ int a2a_sssp_loads(const a2a_topo* topo, int32_t src_begin, int32_t src_count, i
  *   dist       device, int32[src_count][N], and
  *   sigma      device, double[src_count][N]: as a2a_distances leaves them for these sources.  Read only.  (Other
  *              values give other costs, never an access out of bounds.)
- *   link_cost  device, double[E], by link id; any finite numbers.  NULL: 1 for every link
+ *   link_cost  device, double[E], by link id; any finite numbers.  NULL: 1 for every link.  (The costs of all shortest
+ *              paths of a pair together, sigma(s,t) cost(s,t), have to stay within a double, and sigma with them.)
  *   cost       device, double[src_count][N], row-major, overwritten; 0 where t = s or t cannot be reached
  *   workspace  device, a2a_workspace_bytes(topo, src_count, A2A_WS_COSTS) bytes, 256-byte aligned
  * Only enqueues, like a2a_link_loads.  Every sum is taken in a fixed order.
@@ -230,6 +231,7 @@ int a2a_path_costs(const a2a_topo* topo, int32_t src_begin, int32_t src_count, c
  * The all-to-all of a mixture-of-experts layer.  Its tokens lie on hosts, so do its experts, and a router has chosen
  * some experts for every token: that is who sends how much to whom.  The functions below take the router's output as it
  * lies on the device.  They only enqueue, like a2a_link_loads, and their results are the same bits from run to run.
+ * The handle's device has to be the current one (A2A_ERR_INVALID_ARG otherwise, and in a2a_path_costs).
  * They count in whole numbers; logits, probabilities and their sums are single precision.  Sources here are the
  * consecutive groups of tokens that host_begin says: hosts, or for a2a_dispatch_counts and the balance loss whatever a
  * program groups tokens by (sequences, one group for all).
@@ -248,7 +250,8 @@ typedef struct a2a_routing {
   int64_t choices_stride;     /* in numbers, >= choices_per_token */
   const int64_t* host_begin;  /* device, int64[src_count + 1], non-decreasing: source s has the tokens
                                  host_begin[s] .. host_begin[s+1]-1.  Tokens before host_begin[0], from
-                                 host_begin[src_count] on and outside 0 .. tokens-1 belong to no source. */
+                                 host_begin[src_count] on and outside 0 .. tokens-1 belong to no source.
+                                 (Decreasing numbers give other results, never an access out of bounds.) */
   const int32_t* expert_host; /* device, int32[experts]: the host of each expert; a number outside [0, N)
                                  is none, the expert is sent nothing.  NULL: expert e lies on host e. */
 } a2a_routing;

@@ -250,37 +250,52 @@ _torch = None    # the module, once the library is loaded
 _type_codes = {}  # a2a_type of a torch type
 
 
+def _device() -> int:
+    """The current device."""
+    load_library()
+    return _torch._C._cuda_getDevice()
+
+
 def _refuse(where: str, why: str):
     raise A2AError(ERR_INVALID_ARG, f"{where}: {why}")
 
 
-def _whole(where: str, name: str, t, dtype, shape) -> int:
-    """Address of a contiguous device tensor of that type and shape."""
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        _refuse(where, f"{name} has to be a contiguous {dtype} device tensor of shape {tuple(shape)}")
+def _whole(where: str, device: int, name: str, t, dtype, shape) -> int:
+    """Address of a contiguous tensor of that type and shape on the current device."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        _refuse(where, f"{name} has to be a contiguous {dtype} tensor of shape {tuple(shape)} on the current device")
     return t.data_ptr()
 
 
-def _rows(where: str, name: str, t, codes):
+def _workspace(where: str, device: int, t):
+    """Address and bytes of a workspace on the current device."""
+    if t is None:
+        return None, 0
+    if t.get_device() != device or not t.is_contiguous():
+        _refuse(where, "workspace has to be a contiguous tensor on the current device")
+    return t.data_ptr(), t.nbytes
+
+
+def _rows(where: str, device: int, name: str, t, codes):
     """Type and distance of the rows of a device matrix whose numbers lie next to each other in a row."""
     code = _type_codes.get(t.dtype)
-    if code not in codes or not t.is_cuda or t.dim() != 2:
-        _refuse(where, f"{name} has to be a device matrix of one of the types in the header")
+    if code not in codes or t.get_device() != device or t.dim() != 2:
+        _refuse(where, f"{name} has to be a matrix on the current device, of one of the types in the header")
     stride, step = t.stride()
     if step != 1 and t.shape[1] > 1 and t.numel() > 0:
         _refuse(where, f"{name} has to have the numbers of a row next to each other")
     return code, stride if t.shape[0] > 1 else t.shape[1]
 
 
-def _routing(where: str, src_count: int, host_begin, experts: int, expert_host, *, choices=None, tokens=0, choices_per_token=0):
+def _routing(where: str, device: int, src_count: int, host_begin, experts: int, expert_host, *, choices=None, tokens=0, choices_per_token=0):
     kind = at = stride = 0
     if choices is not None:
-        kind, stride = _rows(where, "choices", choices, (3, 4))
+        kind, stride = _rows(where, device, "choices", choices, (3, 4))
         tokens, choices_per_token = choices.shape
         at = choices.data_ptr()
     return Routing(tokens, choices_per_token, experts, kind, 0, at, stride,
-                   _whole(where, "host_begin", host_begin, _torch.int64, (src_count + 1,)),
-                   None if expert_host is None else _whole(where, "expert_host", expert_host, _torch.int32, (experts,)))
+                   _whole(where, device, "host_begin", host_begin, _torch.int64, (src_count + 1,)),
+                   None if expert_host is None else _whole(where, device, "expert_host", expert_host, _torch.int32, (experts,)))
 
 
 def _stream(stream) -> Optional[int]:
@@ -365,32 +380,31 @@ class Topology:
         """a2a_path_costs: ``dist`` and ``sigma`` as :meth:`distances` leaves them, ``link_cost`` float64 [E] (None: 1 each),
         ``cost`` float64 [src_count][N]: mean cost of the shortest paths, the gradient of ``(link_cost * load).sum()`` by
         the demands of :meth:`link_loads_demand` (there by target, here by source)."""
-        where, shape = "a2a_path_costs", (src_count, self.N)
+        where, device, shape = "a2a_path_costs", _device(), (src_count, self.N)
         return _check(load_library().a2a_path_costs(
-            self._h, src_begin, src_count, _whole(where, "dist", dist, _torch.int32, shape),
-            _whole(where, "sigma", sigma, _torch.float64, shape),
-            None if link_cost is None else _whole(where, "link_cost", link_cost, _torch.float64, (self.E,)),
-            _whole(where, "cost", cost, _torch.float64, shape), _ptr(workspace),
-            workspace.numel() if workspace is not None else 0, _stream(stream)), where)
+            self._h, src_begin, src_count, _whole(where, device, "dist", dist, _torch.int32, shape),
+            _whole(where, device, "sigma", sigma, _torch.float64, shape),
+            None if link_cost is None else _whole(where, device, "link_cost", link_cost, _torch.float64, (self.E,)),
+            _whole(where, device, "cost", cost, _torch.float64, shape), *_workspace(where, device, workspace), _stream(stream)), where)
 
     def dispatch_counts(self, src_count: int, *, choices, host_begin, experts: int, counts, stream=None) -> int:
         """a2a_dispatch_counts: how many of the ``choices`` (int32 or int64 [tokens][k]) of each source's tokens fall on
         each expert.  Source s has the tokens ``host_begin[s]`` to ``host_begin[s + 1] - 1`` (int64 [src_count + 1]).
         ``counts``: int32 [src_count][experts]."""
-        where = "a2a_dispatch_counts"
-        r = _routing(where, src_count, host_begin, experts, None, choices=choices)
+        where, device = "a2a_dispatch_counts", _device()
+        r = _routing(where, device, src_count, host_begin, experts, None, choices=choices)
         return _check(load_library().a2a_dispatch_counts(
-            self._h, src_count, r, _whole(where, "counts", counts, _torch.int32, (src_count, experts)), _stream(stream)), where)
+            self._h, src_count, r, _whole(where, device, "counts", counts, _torch.int32, (src_count, experts)), _stream(stream)), where)
 
     def dispatch_demand(self, src_count: int, *, choices, host_begin, experts: int, expert_host=None, once: bool = False,
                         demand, stream=None) -> int:
         """a2a_dispatch_demand: what each source sends to each host, ``demand`` of :meth:`link_loads_demand` (float64
         [N][src_count]), in tokens.  Expert e lies on host ``expert_host[e]`` (int32; None: on host e); ``once``: a token goes
         to a host once, however many of its choices are there."""
-        where = "a2a_dispatch_demand"
-        r = _routing(where, src_count, host_begin, experts, expert_host, choices=choices)
+        where, device = "a2a_dispatch_demand", _device()
+        r = _routing(where, device, src_count, host_begin, experts, expert_host, choices=choices)
         return _check(load_library().a2a_dispatch_demand(
-            self._h, src_count, r, int(once), _whole(where, "demand", demand, _torch.float64, (self.N, src_count)),
+            self._h, src_count, r, int(once), _whole(where, device, "demand", demand, _torch.float64, (self.N, src_count)),
             _stream(stream)), where)
 
     def balance_workspace_bytes(self, src_count: int, *, tokens: int, experts: int) -> int:
@@ -407,38 +421,37 @@ class Topology:
         """a2a_balance_loss: ``loss`` (float32 [1]) of a router with ``logits`` (float32, bfloat16 or float16
         [tokens][experts]) that made ``choices``, weighted by ``cost`` (float64 [src_count][N]; None: 1 each); and, for the
         gradient, ``counts`` (int32 [src_count][experts]), ``prob_sums`` (float32, the same) and ``rows`` (int32 [src_count])."""
-        where = "a2a_balance_loss"
-        kind, stride = _rows(where, "logits", logits, (0, 1, 2))
+        where, device = "a2a_balance_loss", _device()
+        kind, stride = _rows(where, device, "logits", logits, (0, 1, 2))
         tokens, experts = logits.shape
-        r = _routing(where, src_count, host_begin, experts, expert_host, choices=choices)
+        r = _routing(where, device, src_count, host_begin, experts, expert_host, choices=choices)
         if r.tokens != tokens:
             _refuse(where, "logits and choices have to have as many rows")
         shape = (src_count, experts)
         return _check(load_library().a2a_balance_loss(
             self._h, src_count, r, logits.data_ptr(), kind, stride,
-            None if cost is None else _whole(where, "cost", cost, _torch.float64, (src_count, self.N)),
-            _whole(where, "loss", loss, _torch.float32, (1,)), _whole(where, "counts", counts, _torch.int32, shape),
-            _whole(where, "prob_sums", prob_sums, _torch.float32, shape),
-            _whole(where, "rows", rows, _torch.int32, (src_count,)), _ptr(workspace),
-            workspace.numel() if workspace is not None else 0, _stream(stream)), where)
+            None if cost is None else _whole(where, device, "cost", cost, _torch.float64, (src_count, self.N)),
+            _whole(where, device, "loss", loss, _torch.float32, (1,)), _whole(where, device, "counts", counts, _torch.int32, shape),
+            _whole(where, device, "prob_sums", prob_sums, _torch.float32, shape),
+            _whole(where, device, "rows", rows, _torch.int32, (src_count,)), *_workspace(where, device, workspace), _stream(stream)), where)
 
     def balance_loss_grad(self, src_count: int, *, logits, choices_per_token: int, host_begin, cost=None, expert_host=None,
                           counts, rows, upstream=None, grad, stream=None) -> int:
         """a2a_balance_loss_grad: gradient of :meth:`balance_loss` by the logits, ``grad`` (like ``logits``), times
         ``upstream`` (float32 [1]; None: 1)."""
-        where = "a2a_balance_loss_grad"
-        kind, stride = _rows(where, "logits", logits, (0, 1, 2))
-        grad_stride = _rows(where, "grad", grad, (kind,))[1]
+        where, device = "a2a_balance_loss_grad", _device()
+        kind, stride = _rows(where, device, "logits", logits, (0, 1, 2))
+        grad_stride = _rows(where, device, "grad", grad, (kind,))[1]
         tokens, experts = logits.shape
         if grad.shape != logits.shape:
             _refuse(where, "grad has to have the shape of logits")
-        r = _routing(where, src_count, host_begin, experts, expert_host, tokens=tokens, choices_per_token=choices_per_token)
+        r = _routing(where, device, src_count, host_begin, experts, expert_host, tokens=tokens, choices_per_token=choices_per_token)
         return _check(load_library().a2a_balance_loss_grad(
             self._h, src_count, r, logits.data_ptr(), kind, stride,
-            None if cost is None else _whole(where, "cost", cost, _torch.float64, (src_count, self.N)),
-            _whole(where, "counts", counts, _torch.int32, (src_count, experts)),
-            _whole(where, "rows", rows, _torch.int32, (src_count,)),
-            None if upstream is None else _whole(where, "upstream", upstream, _torch.float32, (1,)),
+            None if cost is None else _whole(where, device, "cost", cost, _torch.float64, (src_count, self.N)),
+            _whole(where, device, "counts", counts, _torch.int32, (src_count, experts)),
+            _whole(where, device, "rows", rows, _torch.int32, (src_count,)),
+            None if upstream is None else _whole(where, device, "upstream", upstream, _torch.float32, (1,)),
             grad.data_ptr(), grad_stride, _stream(stream)), where)
 
     def profile_enable(self, mode: int = 1) -> None:

@@ -67,7 +67,8 @@ def test_counts(a2a, shape, dtype, kind):
 @pytest.mark.parametrize("kind", ["even", "ragged", "one", "past"])
 @pytest.mark.parametrize("shape", [
     (64, 64, 96, 2, 64), (1, 1, 9, 2, 3), (81, 81, 3000, 6, 405), (81, 17, 500, 4, 81), (300, 300, 2000, 8, 100),
-    (1000, 1, 3000, 3, 2000), (1030, 9, 4000, 4, 1030), (600, 600, 1, 1, 600), (40, 40, 0, 2, 10), (9000, 20, 700, 5, 9000)])
+    (1000, 1, 3000, 3, 2000), (1030, 9, 4000, 4, 1030), (600, 600, 1, 1, 600), (40, 40, 0, 2, 10), (9000, 20, 700, 5, 9000),
+    (40, 40, 600, 20, 90), (20, 3, 5000, 64, 33), (600, 600, 900, 9, 30), (2100, 2100, 6000, 3, 2100)])
 def test_demand(a2a, shape, kind, once):
     import torch
     N, S, T, k, X = shape
@@ -126,6 +127,96 @@ def test_many_tokens_of_one_pair(a2a):
         want = torch.zeros((4, 4), dtype=torch.float64)
         want[2, 1], want[2, 2] = (T - 1) * (1 if once else k), 1 if once else k
         assert torch.equal(demand.cpu(), want)
+    topo.close()
+
+
+@gpu
+def test_many_choices_of_a_band(a2a):
+    """More than 65535 choices of sources that one workgroup has: cells of 32 bits, and the rows in two halves."""
+    import torch
+    N, T, k = 600, 30000, 4
+    topo = ring(a2a, N)
+    g = torch.Generator("cuda").manual_seed(5)
+    c = torch.randint(-1, N, (T, k), device="cuda", generator=g)
+    begin = torch.zeros(N + 1, dtype=torch.int64, device="cuda")
+    begin[300:] = T - 500  # source 299 has nearly all
+    begin[400:] = T
+    source = torch.searchsorted(begin, torch.arange(T, device="cuda"), right=True) - 1
+    demand = torch.full((N, N), -7.0, dtype=torch.float64, device="cuda")
+    counts = torch.full((N, N), -7, dtype=torch.int32, device="cuda")
+    topo.dispatch_demand(N, choices=c, host_begin=begin, experts=N, demand=demand)
+    topo.dispatch_counts(N, choices=c, host_begin=begin, experts=N, counts=counts)
+    want = torch.bincount((source[:, None] * N + c)[c >= 0], minlength=N * N).view(N, N)
+    assert torch.equal(counts.long(), want) and torch.equal(demand, want.t().double())
+    topo.close()
+
+
+@gpu
+def test_decreasing_begins_stay_in_bounds(a2a):
+    """host_begin that is none: some numbers, no access out of bounds."""
+    import torch
+    g = torch.Generator("cuda").manual_seed(6)
+    S, T, k, X = 300, 2000, 2, 40
+    topo = ring(a2a, S)
+    c = torch.randint(0, X, (T, k), device="cuda", generator=g)
+    z = torch.randn((T, X), device="cuda", generator=g)
+    for sources in (S, 4):
+        begin = torch.randint(-T, 3 * T, (sources + 1,), device="cuda", generator=g)
+        counts = torch.full((sources + 2, X), -7, dtype=torch.int32, device="cuda")
+        demand = torch.full((S + 2, sources), -7.0, dtype=torch.float64, device="cuda")
+        topo.dispatch_counts(sources, choices=c, host_begin=begin, experts=X, counts=counts[1:-1])
+        topo.dispatch_demand(sources, choices=c, host_begin=begin, experts=X, once=True, demand=demand[1:-1])
+        loss, sums = torch.empty(1, device="cuda"), torch.full((sources + 2, X), -7.0, device="cuda")
+        rows = torch.full((sources + 2,), -7, dtype=torch.int32, device="cuda")
+        ws = topo.alloc_balance_workspace(sources, tokens=T, experts=X).zero_()
+        grad = torch.full((T + 2, X), -7.0, device="cuda")
+        topo.balance_loss(sources, logits=z, choices=c, host_begin=begin, loss=loss, counts=counts[1:-1], prob_sums=sums[1:-1],
+                          rows=rows[1:-1], workspace=ws)
+        topo.balance_loss_grad(sources, logits=z, choices_per_token=k, host_begin=begin, counts=counts[1:-1], rows=rows[1:-1],
+                               grad=grad[1:-1])
+        for x in (counts, demand, sums, rows, grad):
+            assert (x[0] == -7).all() and (x[-1] == -7).all()
+    topo.close()
+
+
+@gpu
+def test_two_streams_at_once(a2a):
+    """Counts, demands, loss and gradient of two batches on two streams of one handle, each with its own buffers: what each gives alone."""
+    import torch
+    S, T, k, X = 64, 6000, 4, 96
+    topo = ring(a2a, S)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+
+    def batch(seed):
+        g = torch.Generator("cuda").manual_seed(seed)
+        z = torch.randn((T, X), device="cuda", generator=g)
+        return dict(z=z, c=z.topk(k, dim=1).indices, begin=torch.linspace(0, T, S + 1, device="cuda").long(),
+                    place=torch.randint(0, S, (X,), device="cuda", generator=g, dtype=torch.int32),
+                    ws=topo.alloc_balance_workspace(S, tokens=T, experts=X))
+
+    def call(b, stream=None):
+        f = dict(device="cuda")
+        demand, loss = torch.empty((S, S), dtype=torch.float64, **f), torch.empty(1, **f)
+        counts, sums = torch.empty((S, X), dtype=torch.int32, **f), torch.empty((S, X), **f)
+        rows, grad = torch.empty(S, dtype=torch.int32, **f), torch.empty_like(b["z"])
+        topo.dispatch_demand(S, choices=b["c"], host_begin=b["begin"], experts=X, expert_host=b["place"], demand=demand, stream=stream)
+        w = dict(cost=demand.t().contiguous(), expert_host=b["place"], stream=stream)
+        topo.balance_loss(S, logits=b["z"], choices=b["c"], host_begin=b["begin"], loss=loss, counts=counts, prob_sums=sums, rows=rows,
+                          workspace=b["ws"], **w)
+        topo.balance_loss_grad(S, logits=b["z"], choices_per_token=k, host_begin=b["begin"], counts=counts, rows=rows, grad=grad, **w)
+        return [demand, loss, counts, sums, rows, grad, w["cost"]]
+
+    batches = [batch(1), batch(2)]
+    torch.cuda.synchronize()
+    want = [call(b) for b in batches]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for b, st in zip(batches, streams):
+            with torch.cuda.stream(st):
+                got.append(call(b, st))
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for a, b in zip(got, want) for x, y in zip(a, b))
     topo.close()
 
 

@@ -174,10 +174,9 @@ def test_gradient_of_the_loads_cost(a2a, make):
 def test_other_distances_stay_in_bounds(a2a):
     """Distances and counts of another topology, and numbers that are none: some costs, no access out of bounds."""
     import torch
-    for n, d in ((700, 4), (9000, 3), (20011, 3), (66000, 2)):
+    for n, d, count in ((700, 4, 5), (4000, 4, 5), (8000, 3, 5), (9000, 3, 5), (20011, 3, 5), (20011, 3, 70), (66000, 2, 5)):
         topo = a2a.Topology(*gen.random_regular(n, d, 1))
         g = torch.Generator("cuda").manual_seed(2)
-        count = 5
         dist = torch.randint(-2**31, 2**31 - 1, (count, n), dtype=torch.int32, device="cuda", generator=g)
         dist[1:3] = torch.randint(-3, topo.level_bound + 3, (2, n), dtype=torch.int32, device="cuda", generator=g)
         sigma = torch.randn((count, n), dtype=torch.float64, device="cuda", generator=g)
