@@ -222,7 +222,7 @@ int a2a_sssp_loads(const a2a_topo* topo, int32_t src_begin, int32_t src_count, i
  *              paths of a pair together, sigma(s,t) cost(s,t), have to stay within a double, and sigma with them.)
  *   cost       device, double[src_count][N], row-major, overwritten; 0 where t = s or t cannot be reached
  *   workspace  device, a2a_workspace_bytes(topo, src_count, A2A_WS_COSTS) bytes, 256-byte aligned
- * Only enqueues, like a2a_link_loads.  Every sum is taken in a fixed order.
+ * Only enqueues, like a2a_link_loads.  The same bits from run to run; the last ones may differ for other source ranges.
  */
 int a2a_path_costs(const a2a_topo* topo, int32_t src_begin, int32_t src_count, const int32_t* dist, const double* sigma,
                    const double* link_cost, double* cost, void* workspace, size_t workspace_bytes, void* hip_stream);

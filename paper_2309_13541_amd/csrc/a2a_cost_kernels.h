@@ -20,6 +20,7 @@ struct CostView {
   const double* link_cost;
   double* prices;   // [words of the link table][N][2], if there are link costs: those of a wave's nodes lie next to each other
   uint32_t* lists;  // [workgroups][N]
+  int* picked;      // null, or [kCostPicked][2] what k_cost_pick has found
   unsigned char* levels;  // [sources][N], with the places of the last links
   uint16_t* masks;
   double2* pairs;  // [sources][N] path count and cost
@@ -43,6 +44,16 @@ static __global__ void __launch_bounds__(kBlock) k_cost_prices(CostView c) {
   c.prices[i] = p < c.in_ptr[v + 1] ? c.link_cost[c.in_link[p]] : 0.0;
 }
 
+// Whether more than a sixth of those nodes have several last links: then taking the nodes in order (k_cost_sources) is the faster way.
+__device__ __forceinline__ bool in_order(const CostView& c) {
+  int reached = 0, several = 0;
+  for (int i = 0; i < kCostPicked; ++i) {
+    reached += c.picked[2 * i];
+    several += c.picked[2 * i + 1];
+  }
+  return 6 * several > reached;
+}
+
 // Lanes whose x, of `bits` bits, is this lane's.
 __device__ __forceinline__ uint64_t lanes_like(unsigned x, int bits) {
   uint64_t m = ~0ull;
@@ -56,12 +67,14 @@ __device__ __forceinline__ uint64_t lanes_like(unsigned x, int bits) {
 // A workgroup per source, its state in LDS: an array of doubles that holds path counts, then B, then C; a level byte a
 // node; the nodes in the order of levels, with a bit for each place of the link table that is a last link.  A thread has
 // kNodes nodes for what needs no order.  Places in a level are handed out a wave at a time (an atomic addition a level and
-// wave); their order changes nothing, a node's sum is its own.
+// wave); their order changes nothing, a node's sum is its own.  Bound by vector ALUs and LDS, about half of the time each: 16x16x16
+// torus, all sources, 210 us (336 MB; 3.1 ms with everything in memory).
 constexpr int cost_waves(int words, int nodes) { return nodes <= 4 && words <= 4 ? 8 : 4; }  // a SIMD
 template <int KS, int kNodes>
 __global__ void __launch_bounds__(kCostThreads, cost_waves(KS, kNodes)) k_cost_sources(CostView c) {
   constexpr bool kInLds = cost_list_in_lds(kNodes);
   constexpr int kShift = kNodes < 16 ? 3 : 0;  // ids of the table are 8 x id up to kScaledNodes
+  if (c.picked != nullptr && !in_order(c)) return;
   extern __shared__ __align__(16) unsigned char cost_state[];
   const int N = c.N, T = blockDim.x, pad = (N + 15) / 16 * 16;
   double* const value = (double*)cost_state;
@@ -262,14 +275,43 @@ __device__ __forceinline__ void only_link(const SmallRow<KS>& r, uint32_t mask, 
   for (int j = 1; j < 2 * KS; ++j) from = place == j ? r.template at<0>(j) : from;
 }
 
+// Nodes that kCostPicked of the call's sources reach, and those of them with several last links: a workgroup a source.
+template <int KS>
+__global__ void __launch_bounds__(kCostThreads) k_cost_pick(CostView c) {
+  extern __shared__ __align__(16) unsigned char cost_state[];
+  unsigned char* const level = cost_state;
+  int* const found = (int*)(cost_state + (c.N + 15) / 16 * 16);  // reached, with several last links
+  if (threadIdx.x < 2) found[threadIdx.x] = 0;
+  for (int v = threadIdx.x; v < c.N; v += kCostThreads) {
+    const int d = c.dist[(size_t)blockIdx.x * (c.sources / kCostPicked) * c.N + v];
+    level[v] = (unsigned char)((unsigned)d <= (unsigned)c.depth ? d : kSmallUnseen);
+  }
+  __syncthreads();
+  int reached = 0, several = 0;
+  for (int v = threadIdx.x; v < c.N; v += kCostThreads) {
+    const int l = level[v];
+    SmallRow<KS> r;
+    r.load(c.in, 8 * v);
+    const uint32_t mask = last_links(r, level, l);
+    reached += l - 1u < (unsigned)c.depth;
+    several += l - 1u < (unsigned)c.depth && (mask & (mask - 1)) != 0;
+  }
+  atomicAdd(&found[0], reached);
+  atomicAdd(&found[1], several);
+  __syncthreads();
+  if (threadIdx.x < 2) c.picked[2 * blockIdx.x + threadIdx.x] = found[threadIdx.x];
+}
+
 // A workgroup per source, level bytes and costs in LDS, every level a pass over a thread's nodes; a wave without a node of
 // the level goes on.  What a node needs whose shortest paths have one last link, its start and its cost, is found for all
 // nodes at once before; path counts are wanted only where there are several.  The next source's distances are under way
-// meanwhile.
+// meanwhile.  Bound by memory where most nodes have one last link: all 16384 sources of a generalized Kautz topology of degree 4 1.23 ms,
+// 3.2 GB without the path counts.
 template <int KS>
 __global__ void __launch_bounds__(kCostThreads) k_cost_scan(CostView c) {
   constexpr int kNodes = kCostScanNodes, kAhead = KS <= 4 ? 4 : 1;
   constexpr uint32_t kSeveral = 1u << 31;
+  if (in_order(c)) return;
   extern __shared__ __align__(16) unsigned char cost_state[];
   const int N = c.N;
   double* const value = (double*)cost_state;
@@ -418,7 +460,8 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_marks(CostView c) {
 
 // Then the nodes of one level.  A workgroup has kCostLevelNodes of a source; workgroups go to the 8 XCDs in turn, and those of an
 // XCD have the parts of its sources one after the other, so that the path counts and costs that they gather, 1 MB a source of
-// 65536 nodes, stay in its L2; the two lie beside each other, one request for both.
+// 65536 nodes, stay in its L2; the two lie beside each other, one request for both.  1024 sources of 65536 nodes of degree 8: 4.0 ms, 5.8 by
+// k_cost_scan_memory, which fetches six times as much past L2.  Bound by the lookups of L1, a line a lane.
 template <int KS>
 __global__ void __launch_bounds__(kCostLevelThreads) k_cost_level(CostView c, int l, int parts) {
   const int k = blockIdx.x / kXcd, s = k / parts * kXcd + blockIdx.x % kXcd;

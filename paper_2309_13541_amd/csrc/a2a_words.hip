@@ -185,7 +185,10 @@ void launch_cost_sources(const CostView& cv, int nodes, int workgroups, hipStrea
   const auto launch = [&](auto kernel) { kernel<<<workgroups, cost_threads(cv.N, nodes), cost_lds(cv.N, nodes, cv.depth), st>>>(cv); };
   const auto scan = [&](auto kernel, bool costs) { kernel<<<workgroups, kCostThreads, cost_scan_lds(cv.N, costs), st>>>(cv); };
   switch (nodes) {
-    case 0: return scan(k_cost_scan<KS>, true);
+    case 0:
+      k_cost_pick<KS><<<kCostPicked, kCostThreads, cost_scan_lds(cv.N, false) + 16, st>>>(cv);
+      scan(k_cost_scan<KS>, true);
+      return launch_cost_sources<KS>(cv, kCostScanNodes, workgroups, st);
     case -1: return scan(k_cost_scan_memory<KS>, false);
     case 2: return launch(k_cost_sources<KS, 2>);
     case 4: return launch(k_cost_sources<KS, 4>);

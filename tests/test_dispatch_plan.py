@@ -10,6 +10,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 CHECK = r"""
 #include <cstdio>
+#include "a2a_cost_plan.h"
 #include "a2a_dispatch_plan.h"
 using namespace a2a_dev;
 static int bad = 0;
@@ -105,6 +106,29 @@ int main() {
                         : c.groups != bands * c.tiles || c.lds * 2 < (size_t)c.tile * c.columns * 4) ++bad;
             if (sources * rows < 1ll << 33 && c.groups * c.threads > 0xffffffffll) ++bad;
           }
+  // path costs: what a way takes fits LDS and the workspace
+  for (int N = 2; N <= 65536; N += N < 9000 ? 7 : 131)
+    for (int depth : {1, 7, 16, 17, 100, 253, 254, 5000})
+      for (int words : {0, 2, 3, 4, 5, 8})
+        for (int sources : {1, 63, 64, 512, 513, N}) {
+          const CostWay way = cost_way(N, words, depth, sources);
+          const CostLayout l = cost_layout(N, words, depth, sources);
+          const int nodes = cost_nodes(N, words, depth);
+          bool ok = (way == CostWay::kLevels) == (words == 0 || depth > 253) && l.total >= 256 && l.total % 256 == 0;
+          if (way != CostWay::kLevels) ok = ok && l.lists - l.prices >= (size_t)N * words * 16;
+          if (way == CostWay::kSources)
+            ok = ok && nodes > 0 && cost_threads(N, nodes) <= 1024 && cost_threads(N, nodes) * nodes >= N && cost_lds(N, nodes, depth) <= kSmallLds &&
+                 (cost_list_in_lds(nodes) || l.picked - l.lists >= (size_t)256 * N * 4) && N <= 65535;
+          if (way == CostWay::kScan)
+            ok = ok && nodes == 16 && N <= 16384 && cost_scan_lds(N, true) <= kSmallLds && cost_scan_lds(N, false) + 16 <= kSmallLds &&
+                 l.picked - l.lists >= (size_t)256 * N * 4 && l.total - l.picked >= 128;
+          if (way == CostWay::kScanMemory || way == CostWay::kLevelLaunches) ok = ok && cost_scan_lds(N, false) <= kSmallLds;
+          if (way == CostWay::kLevelLaunches) {
+            const size_t pairs = (size_t)(sources < 512 ? sources : 512) * N;
+            ok = ok && l.masks - l.levels >= pairs && l.pairs - l.masks >= 2 * pairs && l.total - l.pairs >= 16 * pairs;
+          }
+          if (!ok && ++bad < 10) std::printf("path costs: N %d depth %d words %d sources %d\n", N, depth, words, sources);
+        }
   std::printf("%d bad\n", bad);
   return bad != 0;
 }

@@ -126,12 +126,15 @@ def by_levels(rp, col, dist, sigma, w):
                                    ("torus", (2, 5000), 0, 77, 9), ("torus", (40, 41, 42), 0, 500, 20),
                                    ("random", 9000, 10, 0, 100), ("random", 9000, 16, 8900, 64), ("random", 17000, 10, 0, 70),
                                    ("random", 17000, 12, 5, 80), ("random", 16385, 6, 16000, 385), ("random", 40000, 3, 39000, 700),
-                                   ("torus", (128, 128), 0, 0, 40), ("torus", (8, 8, 8, 8), 0, 0, 4096)], ids=str)
+                                   ("torus", (128, 128), 0, 0, 40), ("torus", (8, 8, 8, 8), 0, 0, 4096),
+                                   ("kautz", 12000, 4, 100, 600), ("kautz", 10000, 5, 0, 512), ("kautz", 10000, 7, 9400, 600),
+                                   ("kautz", 8500, 10, 0, 530), ("kautz", 9000, 11, 8000, 700), ("kautz", 16384, 4, 0, 16384),
+                                   ("random", 9000, 4, 0, 600), ("random", 12000, 16, 0, 512)], ids=str)
 def test_larger(a2a, shape):
     """Of every size of a topology's state, a range of sources; against the definition on the device."""
     import torch
     kind, size, d, s0, count = shape
-    rp, col = gen.random_regular(size, d, 5) if kind == "random" else gen.torus(size)
+    rp, col = gen.torus(size) if kind == "torus" else (gen.random_regular if kind == "random" else gen.imase_itoh)(size, d, *[5] * (kind == "random"))
     print(f"case {shape}", flush=True)
     topo = a2a.Topology(rp, col)
     w = torch.rand(topo.E, dtype=torch.float64, device="cuda", generator=torch.Generator("cuda").manual_seed(1)) + 0.01
@@ -174,7 +177,7 @@ def test_gradient_of_the_loads_cost(a2a, make):
 def test_other_distances_stay_in_bounds(a2a):
     """Distances and counts of another topology, and numbers that are none: some costs, no access out of bounds."""
     import torch
-    for n, d, count in ((700, 4, 5), (4000, 4, 5), (8000, 3, 5), (9000, 3, 5), (20011, 3, 5), (20011, 3, 70), (66000, 2, 5)):
+    for n, d, count in ((700, 4, 5), (4000, 4, 5), (8000, 3, 5), (9000, 3, 5), (9000, 3, 520), (20011, 3, 5), (20011, 3, 70), (66000, 2, 5)):
         topo = a2a.Topology(*gen.random_regular(n, d, 1))
         g = torch.Generator("cuda").manual_seed(2)
         dist = torch.randint(-2**31, 2**31 - 1, (count, n), dtype=torch.int32, device="cuda", generator=g)
