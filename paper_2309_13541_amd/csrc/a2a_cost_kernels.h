@@ -4,7 +4,7 @@
 // costs of all shortest paths to v together,
 //   C(v) = B(v) + sum_u C(u),  B(v) = sum_u sigma(u) link_cost(u -> v),
 // over the links u -> v with D(u) = D(v) - 1.  B and which links these are need no cost of any other node: all nodes at
-// once.  The sums need the level before: level by level.  One division at the end.
+// once.  The sums need the level before: level by level.  One reciprocal a node at the end.
 #pragma once
 
 #include "a2a_cost_plan.h"
@@ -64,12 +64,14 @@ __device__ __forceinline__ uint64_t lanes_like(unsigned x, int bits) {
   return m;
 }
 
+// Waves a SIMD: two workgroups of a compute unit where their nodes' registers allow it.
+constexpr int cost_waves(int words, int nodes) { return nodes <= 4 && words <= 4 ? 8 : 4; }
+
 // A workgroup per source, its state in LDS: an array of doubles that holds path counts, then B, then C; a level byte a
 // node; the nodes in the order of levels, with a bit for each place of the link table that is a last link.  A thread has
 // kNodes nodes for what needs no order.  Places in a level are handed out a wave at a time (an atomic addition a level and
 // wave); their order changes nothing, a node's sum is its own.  Bound by vector ALUs and LDS, about half of the time each: 16x16x16
 // torus, all sources, 210 us (336 MB; 3.1 ms with everything in memory).
-constexpr int cost_waves(int words, int nodes) { return nodes <= 4 && words <= 4 ? 8 : 4; }  // a SIMD
 template <int KS, int kNodes>
 __global__ void __launch_bounds__(kCostThreads, cost_waves(KS, kNodes)) k_cost_sources(CostView c) {
   constexpr bool kInLds = cost_list_in_lds(kNodes);

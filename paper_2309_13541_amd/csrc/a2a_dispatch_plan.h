@@ -54,7 +54,7 @@ inline int check_logits(const a2a_routing* r, const void* logits, int type, int6
 // Counts and demands.  A workgroup has a band of sources to itself, reads their tokens and writes their cells once; sources with
 // many tokens are split over workgroups that add to cells set to 0 before.  The first reads and writes everything once, but a source with
 // most of the tokens is one workgroup's; the second is even, but adds a piece's cells one by one.  So few bands are split where each has
-// more than a workgroup reads in some 10 us (65536 x 4 choices of 64 hosts 9.5 us; 20011 x 6 of 81 hosts 7.0 by bands), and counts where
+// more than a workgroup reads in some 10 us (65536 x 4 choices of 64 hosts 9.5 us by bands, 11.4 split), and counts where
 // a piece has four times as many choices as cells (1048576 x 8 of 1024 sources, the largest 8 times the mean, 256 experts: 44 us by
 // bands, 18.5 split).
 constexpr int kDispatchThreads = 1024;
@@ -69,8 +69,11 @@ struct DispatchCut {
 inline DispatchCut dispatch_cut(int64_t sources, int64_t tokens, int64_t choices_per_token, int64_t rows, bool demand) {
   DispatchCut c;
   const int64_t choices = tokens * choices_per_token;
-  // as many sources a band as leave 256 bands
-  while (demand && c.columns < kDispatchColumns && sources >= 512 * c.columns) c.columns *= 2;
+  // As many sources a band as leave 256 bands, or 128 where a row of demands does not end with a line of 64 bytes: bands then share
+  // lines, the more the narrower they are (us with 256 and 128: 4095 hosts, 524288 x 8 choices 51.7, 40.8, 3249 hosts, 2130 x 7 36.1,
+  // 31.2; 2048 hosts, 100000 x 8 10.1, 13.4, 1024 hosts, 4000 x 2 7.5, 8.7).
+  const int64_t each = sources % 8 == 0 ? 512 : 256;
+  while (demand && c.columns < kDispatchColumns && sources >= each * c.columns) c.columns *= 2;
   const int64_t bands = (sources + c.columns - 1) / c.columns;
   // pieces of the split form, with a pass over the rows' cells each
   const int64_t per = std::max<int64_t>((tokens + 1023) / 1024, (1024 + choices_per_token - 1) / choices_per_token);

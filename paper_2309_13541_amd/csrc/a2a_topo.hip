@@ -10,6 +10,9 @@
 //     loads (of those topologies of more than 4096 nodes that do not go the other ways) by the level kernels
 //   - everything else: the level kernels alone (a2a_kernels.h, where their data model is described)
 //
+// Beside them the dispatch of a mixture-of-experts layer: demands from a router's choices and its balance loss (a2a_dispatch_kernels.h),
+// costs of pairs from costs of links (a2a_cost_kernels.h).
+//
 // Level kernels.  A "group" of G source batches (64 sources each) advances level by level together, one kernel
 // launch per level and pass, as many batches as the caller's workspace holds:
 //   bfs    levels 1 .. deepest (the handle knows the deepest level any source reaches), or the search in LDS
