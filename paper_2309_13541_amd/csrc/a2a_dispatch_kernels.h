@@ -20,12 +20,13 @@ struct Routing {
 
 // Entries of host_begin that are at most t: the source of token t is one less.  Of all lanes together, 64 parts of what
 // is left at a time: three steps for up to 262143 sources.
-__device__ __forceinline__ int begun(const int64_t* __restrict__ begin, int entries, long long t) {
-  int lo = 0, hi = entries;
+__device__ __forceinline__ unsigned begun(const int64_t* __restrict__ begin, unsigned entries, long long t) {
+  static_assert(kSearchParts == kWave);
+  unsigned lo = 0, hi = entries;
   while (lo < hi) {
-    const int part = (hi - lo + kWave - 1) / kWave;
-    const int at = min(lo + (lane_id() + 1) * part, hi) - 1;
-    const int whole = __popcll(__ballot(begin[at] <= t && lo + lane_id() * part < hi));
+    const unsigned part = search_part(lo, hi), lane = (unsigned)lane_id();
+    const unsigned at = search_behind(lo, hi, part, lane) - 1;
+    const unsigned whole = (unsigned)__popcll(__ballot(begin[at] <= t && lo + lane * part < hi));
     // all of the parts before the first whose last entry is larger (of a last, shorter part too)
     if (lo + whole * part >= hi) return hi;
     lo += whole * part;
@@ -199,7 +200,7 @@ __global__ void __launch_bounds__(kDispatchThreads) k_dispatch_split(Dispatch d)
       atomicAdd(d.counts + (size_t)s * d.rows + row0 + row, (int)n);
   };
   while (t < end) {
-    const int n = begun(d.r.host_begin, d.r.sources + 1, t);
+    const int n = (int)begun(d.r.host_begin, d.r.sources + 1u, t);
     if (n > d.r.sources) break;
     const long long next = max(min(end, (long long)d.r.host_begin[n]), t + 1);
     if (n > 0) {
@@ -348,14 +349,15 @@ __device__ __forceinline__ void for_pieces(const Routing& r, long long per, F&& 
   long long t = (long long)blockIdx.x * per;
   const long long end = min(t + per, r.tokens);
   if (t >= end) return;
-  int n = begun(r.host_begin, r.sources + 1, t);  // entries that are at most t
-  while (n <= r.sources) {                        // not behind the last source's tokens
-    const long long stop = r.host_begin[n], after = r.host_begin[min(n + 1, r.sources)];
+  const unsigned sources = r.sources;
+  unsigned n = begun(r.host_begin, sources + 1, t);  // entries that are at most t
+  while (n <= sources) {                             // not behind the last source's tokens
+    const long long stop = r.host_begin[n], after = r.host_begin[min(n + 1, sources)];
     const long long next = max(min(end, stop), t + 1);
-    if (n > 0) f(n - 1, t, next);
+    if (n > 0) f((int)(n - 1), t, next);
     t = next;
     if (t >= end) break;
-    n = stop == t && after > t ? n + 1 : begun(r.host_begin, r.sources + 1, t);
+    n = stop == t && after > t ? n + 1 : begun(r.host_begin, sources + 1, t);
   }
 }
 
@@ -578,7 +580,7 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance_grad(Balance b) {
   const int X = b.r.experts;
   const int wave = threadIdx.x / kWave, lane = lane_id() % kLanes, slot = lane_id() / kLanes;
   double n = 0.0;
-  for (int s = threadIdx.x; s < b.r.sources; s += kBalanceThreads) n += b.in_rows[s];
+  for (unsigned s = threadIdx.x; s < (unsigned)b.r.sources; s += kBalanceThreads) n += b.in_rows[s];
   n = block_sum(n, lds64);
   if (threadIdx.x == 0) lds64[kWaves] = n > 0.0 ? (b.upstream ? (double)b.upstream[0] : 1.0) * X / (b.r.k * n) : 0.0;
   __syncthreads();

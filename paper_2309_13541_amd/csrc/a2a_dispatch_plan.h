@@ -60,10 +60,12 @@ inline int check_logits(const a2a_routing* r, const void* logits, int type, int6
 constexpr int kDispatchThreads = 1024;
 constexpr int kDispatchColumns = 16;    // sources of a band at the most: 128 bytes of a row of demands
 constexpr int kDispatchCells = 65536;   // cells of 16 bits: 128 KB of LDS
+constexpr int64_t kLaunchThreads = 0xffffffffll;  // of a launch, at the most
 struct DispatchCut {
   bool split = false;
   int columns = 1, tile = 1, tiles = 1, threads = 256;
-  int64_t per = 0, groups = 0;  // tokens of a workgroup that splits; workgroups
+  int64_t per = 0, groups = 0;  // tokens of a workgroup that splits; workgroups of a launch
+  int64_t sources = 0;          // of a launch: all of them, but for counts of very many
   size_t lds = 0;
 };
 inline DispatchCut dispatch_cut(int64_t sources, int64_t tokens, int64_t choices_per_token, int64_t rows, bool demand) {
@@ -79,21 +81,32 @@ inline DispatchCut dispatch_cut(int64_t sources, int64_t tokens, int64_t choices
   const int64_t per = std::max<int64_t>((tokens + 1023) / 1024, (1024 + choices_per_token - 1) / choices_per_token);
   const int64_t pieces = (tokens + per - 1) / per + sources;
   c.split = bands < 256 ? choices / bands > 16384 : !demand && choices / pieces > 4 * rows;
+  c.sources = sources;
   if (c.split) {
     c.columns = 1;
     c.tile = (int)std::min<int64_t>(rows, kDispatchCells / 4);
     c.tiles = (int)((rows + c.tile - 1) / c.tile);
-    c.per = per;
-    c.groups = (tokens + per - 1) / per * c.tiles;
+    const int64_t most = kLaunchThreads / c.threads / c.tiles;  // pieces of a launch
+    c.per = std::max(per, (tokens + most - 1) / most);
+    c.groups = (tokens + c.per - 1) / c.per * c.tiles;
     c.lds = (size_t)c.tile * 4;
   } else {
     c.tile = (int)std::min<int64_t>(rows, kDispatchCells / c.columns);
     c.tiles = (int)((rows + c.tile - 1) / c.tile);
-    c.groups = bands * c.tiles;
+    if (!demand) c.sources = std::min(sources, kLaunchThreads / c.threads / c.tiles);  // (demands of as many do not fit the memory)
+    c.groups = (c.sources + c.columns - 1) / c.columns * c.tiles;
     c.lds = ((size_t)(c.tile + 1) / 2 * c.columns + 1) * 4;  // of 16 bits each, or of 32 for half of the rows
     if (demand && choices / bands > 1024) c.threads = kDispatchThreads;
   }
   return c;
+}
+
+// The source that a token belongs to is searched for by a wave, 64 parts of what is left, [lo, hi), at a time.  Unsigned: there may be 2^31
+// entries, and the place behind the last part is up to 63 further.
+constexpr unsigned kSearchParts = 64;
+constexpr unsigned search_part(unsigned lo, unsigned hi) { return (hi - lo + kSearchParts - 1) / kSearchParts; }
+constexpr unsigned search_behind(unsigned lo, unsigned hi, unsigned part, unsigned n) {  // the n-th part's end
+  return lo + (n + 1) * part < hi ? lo + (n + 1) * part : hi;
 }
 
 // Passes over logits: a workgroup has `per` consecutive tokens, of as many sources as they belong to.  The tokens of

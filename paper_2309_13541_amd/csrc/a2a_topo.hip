@@ -1287,7 +1287,14 @@ int dispatch(const a2a_topo* t, int32_t src_count, const a2a_routing* routing, i
     }
   }
   const auto launch = [&](auto kernel) {
-    kernel<<<(unsigned)cut.groups, cut.threads, cut.lds, st>>>(d);
+    for (int64_t s0 = 0; s0 < src_count; s0 += cut.sources) {
+      Dispatch part = d;
+      part.r.host_begin += s0;
+      part.r.sources = (int)std::min<int64_t>(cut.sources, src_count - s0);
+      if (counts) part.counts += (size_t)s0 * d.rows;
+      const int64_t groups = part.r.sources == src_count ? cut.groups : (int64_t)part.r.sources * cut.tiles;
+      kernel<<<(unsigned)groups, cut.threads, cut.lds, st>>>(part);
+    }
   };
   const bool wide = routing->choices_type == A2A_I64;
   if (cut.split && counts)
