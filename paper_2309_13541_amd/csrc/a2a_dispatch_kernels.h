@@ -612,11 +612,12 @@ __global__ void __launch_bounds__(kBalanceThreads) k_balance_grad(Balance b) {
 #pragma unroll
       for (int i = 0; i < kValues; ++i) dot = __builtin_fmaf(x[i], c[i], dot);
       dot = over_lanes<kLanes>(dot, [](float a, float b) { return a + b; });
-      const float inv = sum != 0.0f ? __builtin_amdgcn_rcpf(sum) : 0.0f;
+      const bool token = sum != 0.0f;  // 0 otherwise also where the coefficients are no finite numbers
+      const float inv = token ? __builtin_amdgcn_rcpf(sum) : 0.0f;
       dot *= inv;
       R z;
 #pragma unroll
-      for (int i = 0; i < kValues; ++i) z.set(i, x[i] * inv * (c[i] - dot));
+      for (int i = 0; i < kValues; ++i) z.set(i, token ? x[i] * inv * (c[i] - dot) : 0.0f);
       z.store(to, lane, X);
       to += grad_step;
       left -= kStep;
