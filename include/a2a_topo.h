@@ -102,7 +102,8 @@ int a2a_topo_info(const a2a_topo* topo, int32_t* N, int64_t* E, int32_t* dmax, i
  * smallest size the call accepts; otherwise the size at which all sources go at once (fewest
  * kernel launches): all ceil(src_count/64) batches advance together, and link loads of small
  * topologies, where a workgroup takes its sources from the search to their loads, have a row of
- * partial loads for every workgroup.  Any size in between is used as well as it can be.
+ * partial loads for every workgroup.  Any size in between is used as well as it can be.  With the flags of
+ * several calls together it holds each of them, one at a time (A2A_WS_DISTANCES has no bit of its own: take A2A_WS_SIGMA).
  * Returns 0 on bad arguments.  The workspace must be 256-byte aligned.
  */
 size_t a2a_workspace_bytes(const a2a_topo* topo, int32_t src_count, int flags);

@@ -1555,10 +1555,13 @@ int a2a_topo_info(const a2a_topo* t, int32_t* N, int64_t* E, int32_t* dmax, int3
 size_t a2a_workspace_bytes(const a2a_topo* t, int32_t src_count, int flags) {
   if (!t || src_count < 0 || (size_t)src_count > align_up((size_t)t->N, 64)) return 0;
   if (src_count == 0) return 256;
-  if (flags & A2A_WS_COSTS) return cost_workspace_bytes(t, src_count);
   const bool minimal = (flags & A2A_WS_MINIMAL) != 0;
-  const Layout L = make_layout(t, src_count, flags & 0xff, 0, true, minimal);
-  return minimal || !(flags & A2A_WS_LOADS) || !t->small_loads ? L.total : std::max(L.total, small_loads_bytes(t, src_count));
+  const int others = flags & 0xff & ~A2A_WS_COSTS;
+  const size_t costs = flags & A2A_WS_COSTS ? cost_workspace_bytes(t, src_count) : 0;
+  if (costs != 0 && others == 0) return costs;
+  const Layout L = make_layout(t, src_count, others, 0, true, minimal);
+  const size_t most = std::max(costs, L.total);
+  return minimal || !(flags & A2A_WS_LOADS) || !t->small_loads ? most : std::max(most, small_loads_bytes(t, src_count));
 }
 
 int a2a_distances(const a2a_topo* t, int32_t src_begin, int32_t src_count, int32_t* dist, double* sigma,
