@@ -298,6 +298,14 @@ def _routing(where: str, device: int, src_count: int, host_begin, experts: int, 
                    None if expert_host is None else _whole(where, device, "expert_host", expert_host, _torch.int32, (experts,)))
 
 
+def _written(status: int, where: str, *outputs) -> int:
+    """After a call that writes these tensors by their addresses: torch counts them as changed, so that an autograd graph
+    that has saved one refuses to go on with what is there now."""
+    _check(status, where)
+    _torch._C._increment_version(outputs)
+    return status
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:  # (an object for it is most of a microsecond)
         return _torch._C._cuda_getCurrentRawStream(_torch._C._cuda_getDevice()) or None
@@ -381,11 +389,11 @@ class Topology:
         ``cost`` float64 [src_count][N]: mean cost of the shortest paths, the gradient of ``(link_cost * load).sum()`` by
         the demands of :meth:`link_loads_demand` (there by target, here by source)."""
         where, device, shape = "a2a_path_costs", _device(), (src_count, self.N)
-        return _check(load_library().a2a_path_costs(
+        return _written(load_library().a2a_path_costs(
             self._h, src_begin, src_count, _whole(where, device, "dist", dist, _torch.int32, shape),
             _whole(where, device, "sigma", sigma, _torch.float64, shape),
             None if link_cost is None else _whole(where, device, "link_cost", link_cost, _torch.float64, (self.E,)),
-            _whole(where, device, "cost", cost, _torch.float64, shape), *_workspace(where, device, workspace), _stream(stream)), where)
+            _whole(where, device, "cost", cost, _torch.float64, shape), *_workspace(where, device, workspace), _stream(stream)), where, cost)
 
     def dispatch_counts(self, src_count: int, *, choices, host_begin, experts: int, counts, stream=None) -> int:
         """a2a_dispatch_counts: how many of the ``choices`` (int32 or int64 [tokens][k]) of each source's tokens fall on
@@ -393,8 +401,9 @@ class Topology:
         ``counts``: int32 [src_count][experts]."""
         where, device = "a2a_dispatch_counts", _device()
         r = _routing(where, device, src_count, host_begin, experts, None, choices=choices)
-        return _check(load_library().a2a_dispatch_counts(
-            self._h, src_count, r, _whole(where, device, "counts", counts, _torch.int32, (src_count, experts)), _stream(stream)), where)
+        return _written(load_library().a2a_dispatch_counts(
+            self._h, src_count, r, _whole(where, device, "counts", counts, _torch.int32, (src_count, experts)), _stream(stream)),
+            where, counts)
 
     def dispatch_demand(self, src_count: int, *, choices, host_begin, experts: int, expert_host=None, once: bool = False,
                         demand, stream=None) -> int:
@@ -403,9 +412,9 @@ class Topology:
         to a host once, however many of its choices are there."""
         where, device = "a2a_dispatch_demand", _device()
         r = _routing(where, device, src_count, host_begin, experts, expert_host, choices=choices)
-        return _check(load_library().a2a_dispatch_demand(
+        return _written(load_library().a2a_dispatch_demand(
             self._h, src_count, r, int(once), _whole(where, device, "demand", demand, _torch.float64, (self.N, src_count)),
-            _stream(stream)), where)
+            _stream(stream)), where, demand)
 
     def balance_workspace_bytes(self, src_count: int, *, tokens: int, experts: int) -> int:
         return int(load_library().a2a_balance_workspace_bytes(self._h, src_count, tokens, experts))
@@ -420,7 +429,8 @@ class Topology:
                      prob_sums, rows, workspace, stream=None) -> int:
         """a2a_balance_loss: ``loss`` (float32 [1]) of a router with ``logits`` (float32, bfloat16 or float16
         [tokens][experts]) that made ``choices``, weighted by ``cost`` (float64 [src_count][N]; None: 1 each); and, for the
-        gradient, ``counts`` (int32 [src_count][experts]), ``prob_sums`` (float32, the same) and ``rows`` (int32 [src_count])."""
+        gradient, ``counts`` (int32 [src_count][experts]), ``prob_sums`` (float32, the same) and ``rows`` (int32 [src_count]).  Autograd does not
+        record the call, also where the logits require a gradient: that is :meth:`balance_loss_grad`'s, for the program to hand on."""
         where, device = "a2a_balance_loss", _device()
         kind, stride = _rows(where, device, "logits", logits, (0, 1, 2))
         tokens, experts = logits.shape
@@ -428,17 +438,19 @@ class Topology:
         if r.tokens != tokens:
             _refuse(where, "logits and choices have to have as many rows")
         shape = (src_count, experts)
-        return _check(load_library().a2a_balance_loss(
+        return _written(load_library().a2a_balance_loss(
             self._h, src_count, r, logits.data_ptr(), kind, stride,
             None if cost is None else _whole(where, device, "cost", cost, _torch.float64, (src_count, self.N)),
             _whole(where, device, "loss", loss, _torch.float32, (1,)), _whole(where, device, "counts", counts, _torch.int32, shape),
             _whole(where, device, "prob_sums", prob_sums, _torch.float32, shape),
-            _whole(where, device, "rows", rows, _torch.int32, (src_count,)), *_workspace(where, device, workspace), _stream(stream)), where)
+            _whole(where, device, "rows", rows, _torch.int32, (src_count,)), *_workspace(where, device, workspace), _stream(stream)),
+            where, loss, counts, prob_sums, rows)
 
     def balance_loss_grad(self, src_count: int, *, logits, choices_per_token: int, host_begin, cost=None, expert_host=None,
                           counts, rows, upstream=None, grad, stream=None) -> int:
         """a2a_balance_loss_grad: gradient of :meth:`balance_loss` by the logits, ``grad`` (like ``logits``), times
-        ``upstream`` (float32 [1]; None: 1)."""
+        ``upstream`` (float32 [1]; None: 1).  ``grad`` may be ``logits`` themselves; an autograd graph that has saved them then
+        refuses its backward pass, as after any change in place."""
         where, device = "a2a_balance_loss_grad", _device()
         kind, stride = _rows(where, device, "logits", logits, (0, 1, 2))
         grad_stride = _rows(where, device, "grad", grad, (kind,))[1]
@@ -446,13 +458,13 @@ class Topology:
         if grad.shape != logits.shape:
             _refuse(where, "grad has to have the shape of logits")
         r = _routing(where, device, src_count, host_begin, experts, expert_host, tokens=tokens, choices_per_token=choices_per_token)
-        return _check(load_library().a2a_balance_loss_grad(
+        return _written(load_library().a2a_balance_loss_grad(
             self._h, src_count, r, logits.data_ptr(), kind, stride,
             None if cost is None else _whole(where, device, "cost", cost, _torch.float64, (src_count, self.N)),
             _whole(where, device, "counts", counts, _torch.int32, (src_count, experts)),
             _whole(where, device, "rows", rows, _torch.int32, (src_count,)),
             None if upstream is None else _whole(where, device, "upstream", upstream, _torch.float32, (1,)),
-            grad.data_ptr(), grad_stride, _stream(stream)), where)
+            grad.data_ptr(), grad_stride, _stream(stream)), where, grad)
 
     def profile_enable(self, mode: int = 1) -> None:
         """0 off, 1 events around the launches, 2 the same of the level kernels, which then serve every topology, and
