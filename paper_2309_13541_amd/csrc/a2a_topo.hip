@@ -1309,36 +1309,6 @@ int dispatch(const a2a_topo* t, int32_t src_count, const a2a_routing* routing, i
   return A2A_OK;
 }
 
-// f(a row's shape) for `experts` numbers, in pieces of 16 bytes (wide) or single numbers: few lanes have few steps across lanes, but
-// 8 of them or more read whole lines (160 numbers: 4 lanes of 40 23.5 us for 131071 rows, 8 of 24 18.8), and places that
-// a row leaves empty cost as much as the others (16 lanes of 16 for the 160: 19.8).
-template <bool kWide_, int kLanes_, int kValues_>
-struct RowShape {
-  static constexpr bool kWide = kWide_;
-  static constexpr int kLanes = kLanes_, kValues = kValues_;
-};
-template <typename F>
-void by_row(int experts, bool wide, F&& f) {
-  if (!wide) {
-    if (experts <= 128) return f(RowShape<false, 16, 8>{});
-    if (experts <= 512) return f(RowShape<false, 16, 32>{});
-    return f(RowShape<false, 64, 64>{});
-  }
-  if (experts <= 8) return f(RowShape<true, 1, 8>{});
-  if (experts <= 16) return f(RowShape<true, 2, 8>{});
-  if (experts <= 32) return f(RowShape<true, 4, 8>{});
-  if (experts <= 64) return f(RowShape<true, 8, 8>{});
-  if (experts <= 128) return f(RowShape<true, 16, 8>{});
-  if (experts <= 192) return f(RowShape<true, 8, 24>{});
-  if (experts <= 256) return f(RowShape<true, 16, 16>{});
-  if (experts <= 320) return f(RowShape<true, 8, 40>{});
-  if (experts <= 384) return f(RowShape<true, 16, 24>{});
-  if (experts <= 512) return f(RowShape<true, 16, 32>{});
-  if (experts <= 640) return f(RowShape<true, 16, 40>{});
-  if (experts <= 1024) return f(RowShape<true, 16, 64>{});
-  f(RowShape<true, 64, 64>{});
-}
-
 // f(x), x a number of the type
 template <typename F>
 void by_float(int type, F&& f) {
