@@ -93,3 +93,41 @@ def test_counts_of_more_sources_than_a_launch_has():
         assert int(want.sum()) > 0.9 * T  # two of four numbers that a choice may be are experts: one choice a token counts
         assert all(int(p.sum()) > 0.4 * T for p in (want[:16777215], want[16777215:2 * 16777215]))
     topo.close()
+
+
+@pytest.mark.gpu
+def test_most_tokens():
+    """2^31 - 1 choices, the most there may be: counts, demands, the loss and its gradient, by what is known of them."""
+    import torch
+    import paper_2309_13541_amd as a2a
+    f = dict(device="cuda")
+    topo = a2a.Topology(*gen.ring(5))
+    T, S, X = 2**31 - 1, 3, 4
+    c = torch.arange(T, dtype=torch.int32, **f).view(T, 1)
+    c &= 3
+    ends = [0, 1_000_000_001, 1_000_000_004, T]
+    begin = torch.tensor(ends, **f)
+    want = torch.tensor([[(b - e + 3) // 4 - (a - e + 3) // 4 for e in range(X)] for a, b in zip(ends, ends[1:])])
+    counts = torch.empty((S, X), dtype=torch.int32, **f)
+    topo.dispatch_counts(S, choices=c, host_begin=begin, experts=X, counts=counts)
+    assert torch.equal(counts.cpu().long(), want)
+    demand = torch.empty((5, S), dtype=torch.float64, **f)
+    for once in (False, True):
+        topo.dispatch_demand(S, choices=c, host_begin=begin, experts=X, once=once, demand=demand)
+        assert torch.equal(demand[:4].cpu(), want.t().double()) and not demand[4].any()
+    z = torch.zeros((T, X), dtype=torch.bfloat16, **f)  # probability 1/4: every sum is a whole number of quarters below 2^24
+    loss, sums, rows = torch.empty(1, **f), torch.empty((S, X), **f), torch.empty(S, dtype=torch.int32, **f)
+    ws = topo.alloc_balance_workspace(S, tokens=T, experts=X)
+    topo.balance_loss(S, logits=z, choices=c, host_begin=begin, loss=loss, counts=counts, prob_sums=sums, rows=rows, workspace=ws)
+    n = torch.tensor(ends).diff()
+    assert torch.equal(counts.cpu().long(), want) and torch.equal(rows.cpu().long(), n)
+    assert torch.equal(sums.cpu(), (n.double() / 4).float()[:, None].expand(S, X))
+    assert float(loss) == 1.0  # X / n * sum_s (sum_e counts) / rows * rows / 4: all choices
+    up = torch.full((1,), float(T), **f)
+    topo.balance_loss_grad(S, logits=z, choices_per_token=1, host_begin=begin, counts=counts, rows=rows, upstream=up, grad=z)
+    share = want.double() / n[:, None]  # up p (c - mean c) = X / 4 (share - 1/4)
+    for s, t in enumerate([0, 1_000_000_000, 1_000_000_001, 1_000_000_003, 1_000_000_004, T - 1]):
+        r = share[s // 2] - 0.25
+        # six roundings of the coefficient 4 share, two terms' difference, and bfloat16's
+        assert ((z[t].cpu().double() - r).abs() <= 8 * 2.0**-24 * 4 + 2.0**-8 * r.abs()).all()
+    topo.close()
