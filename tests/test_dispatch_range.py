@@ -131,3 +131,58 @@ def test_most_tokens():
         # six roundings of the coefficient 4 share, two terms' difference, and bfloat16's
         assert ((z[t].cpu().double() - r).abs() <= 8 * 2.0**-24 * 4 + 2.0**-8 * r.abs()).all()
     topo.close()
+
+
+@pytest.mark.gpu
+def test_cells_past_32_bits():
+    """More cells than 32 bits count: 600000 groups x 4096 experts, 46600 x 46600 hosts."""
+    import torch
+    import paper_2309_13541_amd as a2a
+    f = dict(device="cuda")
+    g = torch.Generator("cuda").manual_seed(11)
+    topo = a2a.Topology(*gen.ring(3))
+    S, T, k, X = 600_000, 5003, 3, 4096
+    begin = torch.randint(0, T + 1, (S + 1,), generator=g, **f).sort().values
+    begin[-20:] = T
+    begin[:300_000] = 0
+    c = torch.randint(-1, X + 1, (T, k), generator=g, **f)
+    z = torch.full((T, X), -torch.inf, **f)  # all on one expert: probability 1
+    one = torch.randint(0, X, (T,), generator=g, **f)
+    z[torch.arange(T, **f), one] = 2.0
+    source = torch.searchsorted(begin, torch.arange(T, **f), right=True) - 1
+    inside = (source >= 0) & (source < S)
+    on = (c >= 0) & (c < X) & inside[:, None]
+    cells = (source[:, None] * X + c)[on]
+    assert int(cells.max()) > 2**31
+    counts = torch.full((S, X), -7, dtype=torch.int32, **f)
+    topo.dispatch_counts(S, choices=c, host_begin=begin, experts=X, counts=counts)
+
+    def check():
+        assert int(counts.sum(dtype=torch.int64)) == cells.numel()
+        at, n = cells.unique(return_counts=True)
+        assert torch.equal(counts.view(-1)[at].long(), n)
+        assert int((counts != 0).sum()) == at.numel()
+
+    check()
+    sums, rows, loss = torch.full((S, X), -7.0, **f), torch.full((S,), -7, dtype=torch.int32, **f), torch.empty(1, **f)
+    ws = topo.alloc_balance_workspace(S, tokens=T, experts=X)
+    counts.fill_(-7)
+    topo.balance_loss(S, logits=z, choices=c, host_begin=begin, loss=loss, counts=counts, prob_sums=sums, rows=rows, workspace=ws)
+    check()
+    at, n = (source * X + one)[inside].unique(return_counts=True)
+    assert torch.equal(sums.view(-1)[at], n.float()) and int((sums != 0).sum()) == at.numel()
+    assert torch.equal(rows.long(), torch.bincount(source[inside], minlength=S))
+    del counts, sums, ws
+    topo.close()
+    N = 46600
+    topo = a2a.Topology(*gen.imase_itoh(N, 8))
+    begin = torch.linspace(0, T, N + 1, **f).long()
+    begin[-1] = T
+    c = torch.randint(-1, N + 1, (T, k), generator=g, **f)
+    demand = torch.full((N, N), -7.0, dtype=torch.float64, **f)
+    topo.dispatch_demand(N, choices=c, host_begin=begin, experts=N, demand=demand)
+    source = torch.searchsorted(begin, torch.arange(T, **f), right=True) - 1
+    at, n = (c * N + source[:, None])[(c >= 0) & (c < N)].unique(return_counts=True)
+    assert int(at.max()) > 2**31
+    assert torch.equal(demand.view(-1)[at], n.double()) and int((demand != 0).sum()) == at.numel()
+    topo.close()
