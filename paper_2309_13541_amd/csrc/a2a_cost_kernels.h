@@ -70,8 +70,9 @@ constexpr int cost_waves(int words, int nodes) { return nodes <= 4 && words <= 4
 // A workgroup per source, its state in LDS: an array of doubles that holds path counts, then B, then C; a level byte a
 // node; the nodes in the order of levels, with a bit for each place of the link table that is a last link.  A thread has
 // kNodes nodes for what needs no order.  Places in a level are handed out a wave at a time (an atomic addition a level and
-// wave); their order changes nothing, a node's sum is its own.  Bound by vector ALUs and LDS, about half of the time each: 16x16x16
-// torus, all sources, 210 us (336 MB; 3.1 ms with everything in memory).
+// wave); their order changes nothing, a node's sum is its own.  16x16x16 torus, all sources, 210 us (336 MB; 3.1
+// ms with everything in memory): vector ALUs are busy 63 % of the time, LDS about 40 %, with two workgroups a compute unit, all the waves that
+// it takes, and barriers between levels.
 template <int KS, int kNodes>
 __global__ void __launch_bounds__(kCostThreads, cost_waves(KS, kNodes)) k_cost_sources(CostView c) {
   constexpr bool kInLds = cost_list_in_lds(kNodes);
@@ -223,8 +224,8 @@ __global__ void __launch_bounds__(kCostThreads, cost_waves(KS, kNodes)) k_cost_s
 static __device__ const double kCostUnit = 1.0;  // of a link, where the call has no link costs
 
 // Mean over the last links of a node's shortest paths, those that `mask` says, with everything that it takes in flight together:
-// a place without such a link asks for what node 0 has.  (64 lanes with different lines take a request 64 cycles: those that ask for
-// the same one, and prices next to each other, spare most of them.)
+// a place without such a link asks for what node 0 has.  (Lanes that ask for the same line, and prices next to each other, are one lookup in
+// L1: 10 lookups a request of 64 lanes for 65536 nodes of degree 8.)
 // of(u): path count and cost of node u.
 template <int KS, typename F>
 __device__ __forceinline__ double cost_mean(const CostView& c, F&& of, const SmallRow<KS>& r, uint32_t mask, int v) {
@@ -307,8 +308,9 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_pick(CostView c) {
 // A workgroup per source, level bytes and costs in LDS, every level a pass over a thread's nodes; a wave without a node of
 // the level goes on.  What a node needs whose shortest paths have one last link, its start and its cost, is found for all
 // nodes at once before; path counts are wanted only where there are several.  The next source's distances are under way
-// meanwhile.  Bound by memory where most nodes have one last link: all 16384 sources of a generalized Kautz topology of degree 4 1.23 ms,
-// 3.2 GB without the path counts.
+// meanwhile.  Where most nodes have one last link: all 16384 sources of a generalized Kautz topology of degree 4 1.25 ms, 3.2 GB without
+// the path counts, 2.6 TB/s (costs are written in whole lines, 2.16 GB by the counter).  No unit is full: vector ALUs 44 %, L1 73 % with
+// data on its way.  A workgroup of 16 waves is all that LDS has room for, and its phases follow one another.
 template <int KS>
 __global__ void __launch_bounds__(kCostThreads) k_cost_scan(CostView c) {
   constexpr int kNodes = kCostScanNodes, kAhead = KS <= 4 ? 4 : 1;
@@ -463,7 +465,8 @@ __global__ void __launch_bounds__(kCostThreads) k_cost_marks(CostView c) {
 // Then the nodes of one level.  A workgroup has kCostLevelNodes of a source; workgroups go to the 8 XCDs in turn, and those of an
 // XCD have the parts of its sources one after the other, so that the path counts and costs that they gather, 1 MB a source of
 // 65536 nodes, stay in its L2; the two lie beside each other, one request for both.  1024 sources of 65536 nodes of degree 8: 4.0 ms, 5.8 by
-// k_cost_scan_memory, which fetches six times as much past L2.  Bound by the lookups of L1, a line a lane.
+// k_cost_scan_memory, which fetches twice as much past L2 (18 GB).  Bound by what L1 does not have: 275 of 579 million lookups go on to
+// L2, and L1 stands still for it 55 % of the time (lookups alone would take a quarter, the 9.1 GB read and 2.8 written past L2 less than 3 ms).
 template <int KS>
 __global__ void __launch_bounds__(kCostLevelThreads) k_cost_level(CostView c, int l, int parts) {
   const int k = blockIdx.x / kXcd, s = k / parts * kXcd + blockIdx.x % kXcd;

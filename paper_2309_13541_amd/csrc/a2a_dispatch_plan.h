@@ -53,10 +53,12 @@ inline int check_logits(const a2a_routing* r, const void* logits, int type, int6
 
 // Counts and demands.  A workgroup has a band of sources to itself, reads their tokens and writes their cells once; sources with
 // many tokens are split over workgroups that add to cells set to 0 before.  The first reads and writes everything once, but a source with
-// most of the tokens is one workgroup's; the second is even, but adds a piece's cells one by one.  So few bands are split where each has
-// more than a workgroup reads in some 10 us (65536 x 4 choices of 64 hosts 9.5 us by bands, 11.4 split), and counts where
-// a piece has four times as many choices as cells (1048576 x 8 of 1024 sources, the largest 8 times the mean, 256 experts: 44 us by
-// bands, 18.5 split).
+// most of the tokens is one workgroup's; the second is even, but adds a piece's cells one by one, in a second launch.  So few bands are
+// split where they have more than 16384 choices each, by the mean, which is all that the host knows.  How long bands take, the largest source
+// decides (us of a call by bands, split; 64 hosts, k = 4: 65536 tokens, even 8.8, 11.7, the largest source 4 times the mean 10.1, 11.9;
+// 131072 even 8.9, 11.6, 4 times 16.7, 11.7; 262143 even 10.3, 11.8, 4 times, more than cells of 16 bits count, 55.9, 11.7; 81 hosts, 20011 x
+// 6, once, 4 times 9.1, 17.5).  And counts are split where a piece has four times as many choices as cells (1048576 x 8 of 1024 sources, the
+// largest 8 times the mean, 256 experts: 44 us by bands, 18.5 split).
 constexpr int kDispatchThreads = 1024;
 constexpr int kDispatchColumns = 16;    // sources of a band at the most: 128 bytes of a row of demands
 constexpr int kDispatchCells = 65536;   // cells of 16 bits: 128 KB of LDS
